@@ -492,6 +492,110 @@ spqt_status spqt_probe_read(const void* buf, size_t bytes, int pattern,
 spqt_status spqt_probe_arith(int chunks_per_warp, float* sink, size_t sink_floats,
                              unsigned long long* chunks_total, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------------
+ * The rest of a decode step: a cache of keys and values in 8 bits, attention over it, its eviction, and what a caller asks of the
+ * logits.  (No counterpart in the paper, whose path is the linears; these stand between q|k|v and o, and behind the last one.)
+ *
+ * The cache.  A sequence b and a kv head h are a stream of tokens.  It owns blocks of `block_tokens` tokens in a pool, named in
+ * order by its row of `table`: token t lies in pool block table[b][h][t / block_tokens].  A block that is full is held as 8-bit
+ * codes with one fp32 scale for the keys and one for the values: value = code * scale, with
+ *   SPQT_KV_INT8   scale = fp32(max|x| / 127), code = x / scale rounded to the nearest whole number, ties to even
+ *   SPQT_KV_E4M3   scale = fp32(max|x| / 448), code = x / scale rounded to the nearest e4m3 value, ties to even
+ * (one rounding, of the exact quotient; scale 0 for a block of zeros; a block with a value that is not finite holds not-a-number
+ * altogether: its scale is).  The tokens of the block that is not full yet are held as fp16, in `k_tail` and `v_tail`, so that no
+ * token is rounded twice.  `length` counts a stream's tokens: length / block_tokens full blocks, the rest in the tail.
+ * `weight` holds an fp32 value for every token of every block, the attention that the token has received.
+ *
+ * The kernels check what they read of `table` and `length`.  A length that is negative or exceeds the table's row counts as an
+ * empty stream; a block number outside the pool is not followed, and what it stands for is not-a-number.  Either sets the status
+ * word of the workspace to 3 (spqt_kv_status).  Two entries of the table that name one block are not detected.
+ *
+ * Positions are the caller's: keys and queries come as they are to be multiplied (rotated, for instance).
+ */
+enum { SPQT_KV_INT8 = 0, SPQT_KV_E4M3 = 1 };
+
+typedef struct {
+    int batch, kv_heads;  /* streams: batch * kv_heads <= 16384                                                       */
+    int head_dim;         /* 64, 96, 128 or 256                                                                       */
+    int block_tokens;     /* 16, 32, 64 or 128                                                                        */
+    int format;           /* SPQT_KV_INT8, SPQT_KV_E4M3                                                               */
+    int blocks;           /* blocks in the pool                                                                       */
+    int table_width;      /* blocks a stream may own: 1 .. 16384                                                      */
+    void *k_codes, *v_codes;   /* [blocks][block_tokens][head_dim] bytes, 16-byte aligned                             */
+    float *k_scale, *v_scale;  /* [blocks]                                                                            */
+    void *k_tail, *v_tail;     /* fp16 [batch][kv_heads][block_tokens][head_dim], 16-byte aligned                     */
+    int32_t* table;            /* [batch][kv_heads][table_width]                                                      */
+    int32_t* length;           /* [batch][kv_heads]                                                                   */
+    float* weight;             /* [blocks][block_tokens], 16-byte aligned; NULL: not kept                             */
+} spqt_kv_cache;
+
+/*
+ * New tokens: token i < n of sequence b is row k + b * batch_stride + i * token_stride (in fp16 values; kv_heads * head_dim of
+ * them, the heads side by side; 16-byte aligned, strides multiples of 8), the same for v.  n is counts[b], or `tokens` where
+ * counts (int32[batch] on the device) is NULL; a count outside 0 .. tokens counts as 0 and sets the status word.  Blocks that
+ * become full are rounded, the rest stays in the tail, the tokens' weights become 0, and the new lengths go to `length_out`
+ * (int32[batch][kv_heads]; NULL: in place of the old ones).  A stream whose tokens would not fit its row of the table, or of whose
+ * touched blocks one lies outside the pool, is left as it was, and the status word says so.
+ */
+spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void* v, int tokens, long long batch_stride,
+                           long long token_stride, const int32_t* counts, int32_t* length_out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * The cache as fp16, code * scale rounded once: token t of stream (b, h) to k + b * batch_stride + t * token_stride +
+ * h * head_stride (16-byte aligned, strides multiples of 8), the same for v.  Tokens from `tokens` on are left out, rows behind a
+ * stream's last token stay as they were.  `length` NULL: the cache's.
+ */
+spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void* k, void* v, int tokens, long long batch_stride,
+                         long long token_stride, long long head_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that the cache's calls need with at most `q_heads` and `queries` (q_heads a multiple of kv_heads). */
+spqt_status spqt_kv_workspace(const spqt_kv_cache* cache, int q_heads, int queries, size_t* bytes);
+
+/*
+ * Attention of the last `queries` (1 .. 16) tokens of every sequence over the cache, which holds these tokens already.  Query
+ * i of head g (which reads kv head g / (q_heads / kv_heads)) is q + b * q_batch_stride + i * q_token_stride + g * head_dim; it sees
+ * the tokens t < length - queries + 1 + i of its stream:
+ *   out = sum_t p_t v_t,  p = softmax over t of scale * <q, k_t>
+ * at out + b * out_batch_stride + i * out_token_stride + g * head_dim (16-byte aligned, strides multiples of 8).  A query that sees
+ * no token gives zeros.  accumulate != 0: weight of token t += the sum of p_t over the queries and over the query heads of its kv
+ * head (one call adds to each weight once, so that the sums do not depend on an order).  Sums and the softmax are held in fp32, p
+ * enters the product to 2^-22 of the largest.  At most 64 query heads per kv head.
+ *   workspace : spqt_kv_workspace bytes, 16-byte aligned, zeroed once by the caller.  Calls that may overlap need two.
+ */
+spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long long q_batch_stride, long long q_token_stride, int q_heads,
+                              int queries, float scale, int accumulate, void* out, long long out_batch_stride,
+                              long long out_token_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction: of each stream's full blocks stay the `first` first ones, the `recent` last ones and, up to `keep` in all, those with
+ * the largest accumulated weight (the sum of a block's weights in fp64, rounded to fp32; of equal ones the earlier block; a sum
+ * that is not-a-number counts as the largest), in their order.  A stream of at most `keep` full blocks stays as it is.  Nothing but
+ * the table and the length change: the row lists the blocks that stay, then the one that is not full, then those that left, in
+ * their order, ready for the tokens to come, then the rest.  `table_out`, `length_out` NULL: in place.  0 <= first, recent;
+ * first + recent <= keep.
+ */
+spqt_status spqt_kv_evict(const spqt_kv_cache* cache, int keep, int first, int recent, int32_t* table_out, int32_t* length_out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Reads the workspace's status word of the calls above (waits for the stream; see spqt_workspace_status): 0, or 3 for contents of
+ * the cache that were refused (returns SPQT_ERR_INVALID_ARG).  Sticky until the caller zeroes the workspace again. */
+spqt_status spqt_kv_status(const void* workspace, int* status_host, void* stream);
+
+/*
+ * What a row of logits says about a token, without writing probabilities: with lse = log sum_v exp(x[v]) per row,
+ *   logprob[r] = x[tokens[r]] - lse,  entropy[r] = -sum_v p_v log p_v,
+ *   top_logprob[r][i], top_index[r][i], i < top: the largest log probabilities and their places, descending, of equal logits the
+ *   lower place first.
+ * Sums in fp32.  logits: rows of `vocab` values, `row_stride` values apart, aligned to their type.  `tokens` NULL: no logprob; a
+ * token outside [0, vocab) gives not-a-number.  entropy NULL: not computed.  A logit of -infinity has probability 0; a row with
+ * not-a-number, +infinity, or -infinity alone gives not-a-number (the places are still those of the largest logits, not-a-number
+ * above all).  top <= 32, top <= vocab <= 1048576.
+ */
+enum { SPQT_LOGITS_FP16 = 0, SPQT_LOGITS_BF16 = 1, SPQT_LOGITS_FP32 = 2 };
+spqt_status spqt_token_logprobs(const void* logits, int dtype, int rows, int vocab, long long row_stride, const int32_t* tokens, int top,
+                                float* logprob, float* entropy, float* top_logprob, int32_t* top_index, void* stream);
+
 /* Number of kernels the library has launched in this process (a counter for
  * benchmarks; not synchronised with the device). */
 unsigned long long spqt_launch_count(void);

@@ -24,6 +24,7 @@ EXPORTS = (
     "spqt_status_string", "spqt_version", "spqt_packed_sizes", "spqt_pack", "spqt_unpack",
     "spqt_sparsify", "spqt_sparse_gemv", "spqt_sparse_gemv_static", "spqt_static_status", "spqt_sparsify_gemv", "spqt_dense_gemv",
     "spqt_sparse_linear_host", "spqt_sparse_linear_host_async", "spqt_host_step_create", "spqt_host_step_launch", "spqt_host_step_destroy", "spqt_gemm_small_workspace", "spqt_sparse_gemm_small", "spqt_dense_gemm_small", "spqt_rowwise_packed_sizes", "spqt_rowwise_pack", "spqt_rowwise_dense_gemv", "spqt_rowwise_thresholded_gemv", "spqt_kq_packed_sizes", "spqt_kq_pack", "spqt_kq_sparse_gemv", "spqt_kq_dense_gemv", "spqt_kqw_packed_sizes", "spqt_kqw_pack", "spqt_kqw_sparse_gemv", "spqt_kqw_dense_gemv", "spqt_autotune", "spqt_calibrate_threshold", "spqt_set_tuning", "spqt_set_debug", "spqt_workspace_status", "spqt_probe_read", "spqt_probe_arith", "spqt_launch_count",
+    "spqt_kv_append", "spqt_kv_read", "spqt_kv_workspace", "spqt_kv_attention", "spqt_kv_evict", "spqt_kv_status", "spqt_token_logprobs",
 )
 
 _lib = None
@@ -99,6 +100,17 @@ def lib() -> ctypes.CDLL:
         L.spqt_probe_arith.restype = i32
         L.spqt_workspace_status.argtypes = [vp, i32, i32, ctypes.POINTER(i32), vp]
         L.spqt_launch_count.restype = ctypes.c_ulonglong
+        ll = ctypes.c_longlong
+        L.spqt_kv_append.argtypes = [vp, vp, vp, i32, ll, ll, vp, vp, vp, sz, vp]
+        L.spqt_kv_read.argtypes = [vp, vp, vp, vp, i32, ll, ll, ll, vp, sz, vp]
+        L.spqt_kv_workspace.argtypes = [vp, i32, i32, ctypes.POINTER(sz)]
+        L.spqt_kv_attention.argtypes = [vp, vp, ll, ll, i32, i32, ctypes.c_float, i32, vp, ll, ll, vp, sz, vp]
+        L.spqt_kv_evict.argtypes = [vp, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.spqt_kv_status.argtypes = [vp, ctypes.POINTER(i32), vp]
+        L.spqt_token_logprobs.argtypes = [vp, i32, i32, i32, ll, vp, i32, vp, vp, vp, vp, vp]
+        for name in ("spqt_kv_append", "spqt_kv_read", "spqt_kv_workspace", "spqt_kv_attention", "spqt_kv_evict", "spqt_kv_status",
+                     "spqt_token_logprobs"):
+            getattr(L, name).restype = i32
         for name in ("spqt_packed_sizes", "spqt_pack", "spqt_unpack", "spqt_sparsify",
                      "spqt_sparse_gemv", "spqt_dense_gemv", "spqt_sparse_linear_host", "spqt_set_tuning",
                      "spqt_set_debug", "spqt_workspace_status", "spqt_probe_read"):
@@ -528,3 +540,118 @@ def spqt_static_status(m: int, group: int = 128, stream=None) -> int:
 
 def spqt_launch_count() -> int:
     return int(lib().spqt_launch_count())
+
+
+# ---------------------------------------------------------------- the 8-bit cache, attention over it, logits
+
+
+class KVCacheDesc(ctypes.Structure):
+    """spqt_kv_cache of the header."""
+    _fields_ = [(name, ctypes.c_int) for name in ("batch", "kv_heads", "head_dim", "block_tokens", "format", "blocks", "table_width")] + \
+               [(name, ctypes.c_void_p) for name in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "table", "length", "weight")]
+
+
+KV_FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+
+
+class KVCache:
+    """Keys and values of a layer in 8 bits with a scale per block of tokens and head (the layout is in the header): a handle of
+    the tensors it is made of, which it keeps and the caller may read and write, but not replace.
+
+    k_codes, v_codes  int8 or float8_e4m3fn [blocks][block_tokens][head_dim]: the pool
+    k_scale, v_scale  float32 [blocks]
+    k_tail, v_tail    float16 [batch][kv_heads][block_tokens][head_dim]: the tokens of the block that is not full
+    table             int32 [batch][kv_heads][table_width]: the blocks of each stream in order, set by the caller
+    length            int32 [batch][kv_heads]: tokens of each stream
+    weight            float32 [blocks][block_tokens] or None: the attention that each token has received
+    """
+    TENSORS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "table", "length", "weight")
+    __slots__ = tuple("_" + name for name in TENSORS) + ("_desc", "desc", "device_index")
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, table, length, weight=None):
+        if not isinstance(k_codes, torch.Tensor) or k_codes.dtype not in KV_FORMATS or k_codes.dim() != 3:
+            raise TypeError("k_codes must be an int8 or float8_e4m3fn tensor [blocks][block_tokens][head_dim]")
+        if not isinstance(table, torch.Tensor) or table.dim() != 3:
+            raise TypeError("table must be an int32 tensor [batch][kv_heads][table_width]")
+        blocks, block_tokens, head_dim = k_codes.shape
+        batch, kv_heads, table_width = table.shape
+        f32, f16, i32 = torch.float32, torch.float16, torch.int32
+        wanted = {"k_codes": (k_codes, k_codes.dtype, k_codes.shape), "v_codes": (v_codes, k_codes.dtype, k_codes.shape),
+                  "k_scale": (k_scale, f32, (blocks,)), "v_scale": (v_scale, f32, (blocks,)),
+                  "k_tail": (k_tail, f16, (batch, kv_heads, block_tokens, head_dim)),
+                  "v_tail": (v_tail, f16, (batch, kv_heads, block_tokens, head_dim)),
+                  "table": (table, i32, table.shape), "length": (length, i32, (batch, kv_heads)), "weight": (weight, f32, (blocks, block_tokens))}
+        d = KVCacheDesc(batch, kv_heads, head_dim, block_tokens, KV_FORMATS[k_codes.dtype], blocks, table_width)
+        for name, (t, dtype, shape) in wanted.items():
+            if name != "weight" or t is not None:
+                setattr(d, name, _dev(t, dtype, name))
+                if tuple(t.shape) != tuple(shape):
+                    raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+                if t.device != k_codes.device:
+                    raise ValueError("%s must be on the device of k_codes" % name)
+            setattr(self, "_" + name, t)
+        self._desc, self.desc, self.device_index = d, ctypes.addressof(d), k_codes.device.index
+
+    @classmethod
+    def new(cls, batch, kv_heads, head_dim, block_tokens, blocks, table_width, dtype=torch.int8, weight=False, device=None):
+        """An empty cache; ``table`` holds -1 until the caller gives the streams their blocks."""
+        kw = dict(device=device or "cuda")
+        codes, tail = (blocks, block_tokens, head_dim), (batch, kv_heads, block_tokens, head_dim)
+        return cls(*(torch.zeros(codes, dtype=torch.uint8, **kw).view(dtype) for _ in range(2)), *(torch.zeros(blocks, **kw) for _ in range(2)),
+                   *(torch.zeros(tail, dtype=torch.float16, **kw) for _ in range(2)),
+                   torch.full((batch, kv_heads, table_width), -1, dtype=torch.int32, **kw), torch.zeros((batch, kv_heads), dtype=torch.int32, **kw),
+                   torch.zeros((blocks, block_tokens), **kw) if weight else None)
+
+
+for _name in KVCache.TENSORS:
+    setattr(KVCache, _name, property(lambda self, _n="_" + _name: getattr(self, _n)))
+
+
+def new_kv_workspace(cache: KVCache, q_heads: int, queries: int = 1) -> torch.Tensor:
+    """Zeroed workspace of the cache's calls with at most these queries (zeroed once; calls that may overlap need two)."""
+    out = ctypes.c_size_t(0)
+    _ok(lib().spqt_kv_workspace(cache.desc, q_heads, queries, ctypes.byref(out)), "spqt_kv_workspace")
+    return torch.zeros(int(out.value), dtype=torch.uint8, device=cache.k_codes.device)
+
+
+def spqt_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, workspace: torch.Tensor, counts: torch.Tensor = None,
+                   length_out: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """Adds k and v (float16 [batch][tokens][kv_heads][head_dim], the heads of a token side by side) to the cache -> the new
+    lengths.  ``counts``: int32 [batch], how many of the tokens each sequence has; ``length_out``: where the lengths go instead of
+    ``cache.length``."""
+    native().kv_append(cache, k, v, workspace, counts, length_out, stream)
+    return cache.length if length_out is None else length_out
+
+
+def spqt_kv_read(cache: KVCache, k: torch.Tensor, v: torch.Tensor, workspace: torch.Tensor, length: torch.Tensor = None, stream=None) -> None:
+    """Writes the cache as float16 to k and v, [batch][tokens][kv_heads][head_dim] with any strides but a row's; what lies behind a
+    stream's last token stays as it was."""
+    native().kv_read(cache, k, v, workspace, length, stream)
+
+
+def spqt_kv_attention(cache: KVCache, q: torch.Tensor, workspace: torch.Tensor, scale: float = None, accumulate: bool = False,
+                      out: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """Attention of the last tokens' queries (float16 [batch][queries][q_heads][head_dim]) over the cache -> out, of q's shape.
+    ``scale``: head_dim ** -0.5 if not given; ``accumulate``: the probabilities are added to ``cache.weight``."""
+    return native().kv_attention(cache, q, workspace, scale, accumulate, out, stream)
+
+
+def spqt_kv_evict(cache: KVCache, keep: int, workspace: torch.Tensor, first: int = 0, recent: int = 0, table_out: torch.Tensor = None,
+                  length_out: torch.Tensor = None, stream=None):
+    """Of each stream's full blocks stay ``keep``: the ``first`` first, the ``recent`` last, and those with the largest
+    accumulated weight -> (table, length), in place where no other tensors are given."""
+    native().kv_evict(cache, keep, first, recent, workspace, table_out, length_out, stream)
+    return cache.table if table_out is None else table_out, cache.length if length_out is None else length_out
+
+
+def spqt_kv_status(workspace: torch.Tensor, stream=None) -> int:
+    """The status word of the cache's calls: 0, or 3 where contents of the cache were refused.  Synchronises."""
+    out = ctypes.c_int(-1)
+    rc = lib().spqt_kv_status(_dev(workspace, torch.uint8, "workspace"), ctypes.byref(out), _stream(stream))
+    return _status_word(rc, out, "spqt_kv_status")
+
+
+def spqt_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor = None, top: int = 0, entropy: bool = True, stream=None):
+    """-> (log probability of each row's token or None, entropy or None, the ``top`` largest log probabilities, their places);
+    logits [rows][vocab] in float16, bfloat16 or float32, tokens int32 [rows]."""
+    return native().token_logprobs(logits, tokens, top, entropy, stream)

@@ -1,0 +1,866 @@
+// Attention of a step's queries over the 8-bit cache.
+//
+// out = sum_t p_t v_t with p = softmax_t(scale * <q, k_t>), k and v = code * scale of their block.  What bounds it is the codes,
+// 2 * head_dim bytes a token, read once: the query heads of a kv head and the queries of a step are rows of one product.
+//
+// The product runs transposed on mma.sync.m16n8k16: A is the codes, 16 tokens (or 16 dimensions of v) an instruction, B the
+// queries (or the probabilities), eight rows; with few rows the tensor cores are there for their operand format, and the other
+// orientation would fill its 16 rows with nothing.  tcgen05 does not fit: codes would have to be widened to 16 bits through
+// shared memory first, twice the bytes of the codes themselves in and out again.  An 8-bit code becomes an exact fp16 value in
+// registers (a byte permutation and a subtraction, or one conversion from e4m3).  Scales stay outside of the product: a block's k scale multiplies its scores,
+// its v scale the probabilities.
+//
+// Probabilities are needed in fp16: p = 2^(s + e - M + 14), s the score in powers of two, 2^e the power of two in the v scale, M the
+// largest s + e so far.  p then lies in 0 .. 2^14, and what 16 bits cannot hold of it (2^-11) enters as a second fp16 value: with up
+// to four rows in the columns that they leave free, else in a second instruction.  Without it the result is 1.4 times as far from
+// the exact one, as far as its own rounding to fp16 takes it.  Sums are fp32 and know nothing of v's scales.
+//
+// Work: the tiles (32 tokens) of all streams are laid end to end and cut into equal parts, one per CTA; the warps of a CTA take its
+// tiles in turn, each with a ring of tiles on their way (cp.async, so that a block number is all that is needed ahead).  A stream
+// that lies within one CTA is finished there; the others' parts meet in a second kernel, which adds them in the order of the CTAs
+// and, where asked, turns the scores that the first one left into probabilities and adds them to the tokens' weights.
+#include <cuda_fp8.h>
+
+#include "spqt_common.cuh"
+#include "spqt_gemv_device.cuh"
+#include "spqt_mma.cuh"
+#include "spqt_kv.cuh"
+
+namespace spqt {
+
+constexpr int kTile = 32;               // tokens of a tile of codes; half as many of the block that is not full
+constexpr int kMaxAttnCtas = 320;       // parts at most
+constexpr int kLengthCache = 1024;      // streams whose lengths a CTA keeps in shared memory
+constexpr float kUp = 14.0f;            // p of the largest score is 2^kUp
+
+struct AttnArgs {
+    spqt_kv_cache c;
+    const __half* q;
+    long long q_batch, q_token;
+    __half* out;
+    long long out_batch, out_token;
+    int group, queries, rows;           // rows = group * queries of a stream, row i * group + g
+    int row_groups;                     // of ROWS rows
+    int accumulate;
+    float scale_log2;
+    int* status;
+    int* begin;                         // workspace: the first tile of every segment (a stream's row group), behind them their sum
+    float2* ml;                         // parts: (M, l) of every row
+    float* o;                           // parts: sums of every row, not divided yet
+    float* scores;                      // tiles: [kTile][ROWS], in powers of two
+};
+
+template <int D, int ROWS>
+struct AttnShape {
+    static constexpr int kWarps = D == 256 ? 4 : 8;
+    static constexpr int kTileBytes = 2 * kTile * D;
+    static constexpr int kStages = D == 64 ? 4 : (D >= 128 && ROWS == 16) ? 2 : 3;
+    static constexpr int kCols = ROWS == 16 ? 2 : 1;             // sets of eight columns
+    static constexpr int kStride = D + 4;                        // of a row of sums in shared memory: 8 bytes a lane without conflicts
+};
+
+// Tiles of a stream of n tokens: full blocks by 32 tokens, then the open one by 16.
+__device__ __forceinline__ int code_tiles(int n, int bt) { return (n / bt * bt + kTile - 1) / kTile; }
+__device__ __forceinline__ int tiles_of(int n, int bt) { return code_tiles(n, bt) + (n % bt + 15) / 16; }
+
+// CTAs that work: not more than leave a tile for every warp.  A CTA's tiles begin at total * i / ctas.
+__device__ __forceinline__ int working_ctas(long long total, int warps, int most)
+{
+    const long long c = (total + warps - 1) / warps;
+    return (int)(c < most ? (c < 1 ? 1 : c) : most);
+}
+__device__ __forceinline__ int owner_of(long long tile, long long total, int ctas) { return (int)(((tile + 1) * ctas - 1) / total); }
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Four codes of a register as fp16: bytes (0, 1) and (2, 3), or (0, 2) and (1, 3).
+template <int FMT, bool SPREAD>
+__device__ __forceinline__ void widen(unsigned w, unsigned& x, unsigned& y)
+{
+    if (FMT == SPQT_KV_INT8) {
+        const unsigned u = w ^ 0x80808080u;              // code + 128 under the exponent of 1024: 1152 + code
+        const __half2 bias = __half2half2(__ushort_as_half(0x6480));
+        unsigned a = __byte_perm(u, 0x64646464u, SPREAD ? 0x4240 : 0x4140), b = __byte_perm(u, 0x64646464u, SPREAD ? 0x4341 : 0x4342);
+        const __half2 ha = __hsub2(*reinterpret_cast<__half2*>(&a), bias), hb = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
+        x = *reinterpret_cast<const unsigned*>(&ha);
+        y = *reinterpret_cast<const unsigned*>(&hb);
+    } else {
+        const unsigned u = SPREAD ? __byte_perm(w, 0u, 0x3120) : w;
+        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(x), "=r"(y) : "r"(u));
+    }
+}
+
+__device__ __forceinline__ void ldsm_x4(unsigned addr, unsigned* r)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ unsigned transposed(unsigned v)
+{
+    unsigned r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ unsigned halves(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const unsigned*>(&h);
+}
+// 16 bytes, or zeros
+__device__ __forceinline__ void cp_async_16_if(bool on, unsigned dst, const void* src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_scale(unsigned dst, const void* src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+template <int FMT, int D, int ROWS>
+__global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attention_kernel(const AttnArgs a, int streams)
+{
+    using S = AttnShape<D, ROWS>;
+    constexpr int NW = S::kWarps, STAGES = S::kStages, NC = S::kCols, CH = D / 16;
+    extern __shared__ __align__(128) unsigned char s_ring[];                 // [NW][STAGES][kTileBytes]
+    __shared__ int s_len[kLengthCache];
+    __shared__ int s_scan[NW], s_start[2];
+    __shared__ __align__(16) float s_scale[NW][STAGES][4];                   // k scale of the halves, v scale of the halves
+    __shared__ float2 s_ml[NW][ROWS];
+    __shared__ __align__(16) float s_o[NW / 2][ROWS][S::kStride];
+    const spqt_kv_cache& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, cc = lane & 3;
+    const int bt = c.block_tokens;
+    const unsigned ring = smem_u32(s_ring) + warp * STAGES * S::kTileBytes;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- which tiles are this CTA's
+    const int per = (streams + NW * 32 - 1) / (NW * 32);
+    int mine = 0;
+    for (int i = 0; i < per; ++i) {
+        const int st = tid * per + i;
+        if (st < streams) {
+            const int n = length_or_none((int)ld_global_u32(c.length + st), c, a.status);
+            if (st < kLengthCache) s_len[st] = n;
+            mine += tiles_of(n, bt) * a.row_groups;
+        }
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    int base = incl - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        base += w < warp ? s_scan[w] : 0;
+        total += s_scan[w];
+    }
+    auto length_of = [&](int st) { return st < kLengthCache ? s_len[st] : length_or_none((int)ld_global_u32(c.length + st), c, a.status); };
+    const int ctas = working_ctas(total, NW, gridDim.x), cta = blockIdx.x;
+    if (cta == 0) {                           // for the second kernel
+        if (tid == 0) a.begin[streams * a.row_groups] = total;
+        for (int st = tid * per, at = base; st < min(streams, (tid + 1) * per); ++st) {
+            const int k = tiles_of(length_of(st), bt);
+            for (int r = 0; r < a.row_groups; ++r, at += k) a.begin[st * a.row_groups + r] = at;
+        }
+    }
+    if (total == 0 || cta >= ctas) return;
+    const int t0 = (int)((long long)total * cta / ctas), t1 = (int)((long long)total * (cta + 1) / ctas);
+    if (t0 >= base && t0 < base + mine) {
+        int st = tid * per, at = base;
+        for (;; ++st) {
+            const int k = tiles_of(length_of(st), bt) * a.row_groups;
+            if (t0 < at + k) break;
+            at += k;
+        }
+        s_start[0] = st;
+        s_start[1] = at;
+    }
+    __syncthreads();
+    const int stream0 = s_start[0], n0 = length_of(stream0), tiles0 = tiles_of(n0, bt), rg0 = (t0 - s_start[1]) / tiles0;
+    const int seg0 = stream0 * a.row_groups + rg0, begin0 = s_start[1] + rg0 * tiles0;
+
+    // ---- the tiles ahead: a walk over this warp's tiles that knows the segment of each; first the block numbers, one tile later
+    // the copies
+    int w_tile = t0 + warp, w_seg = seg0, w_begin = begin0, w_n = n0, w_end = begin0 + tiles0;
+    auto seek = [&]() {                       // the segment of w_tile
+        while (w_tile >= w_end && w_tile < t1) {
+            ++w_seg;
+            w_begin = w_end;
+            w_n = length_of(w_seg / a.row_groups);
+            w_end = w_begin + tiles_of(w_n, bt);
+        }
+    };
+    seek();
+    int p_tile = w_tile, p_stream = 0, p_local = 0, p_n = 0, p_id = 0;     // the tile whose block numbers are on their way (lane u: half u)
+    auto look_up = [&]() {
+        p_tile = w_tile;
+        if (w_tile < t1) {
+            p_stream = w_seg / a.row_groups;
+            p_local = w_tile - w_begin;
+            p_n = w_n;
+            const int token = p_local * kTile + (lane & 1) * 16;
+            p_id = token < w_n / bt * bt ? (int)ld_global_u32(c.table + (size_t)p_stream * c.table_width + token / bt) : 0;
+            w_tile += NW;
+            seek();
+        }
+    };
+    auto copy = [&](int stage) {
+        if (p_tile >= t1) return;
+        const unsigned dst = ring + stage * S::kTileBytes;
+        const int full = p_n / bt * bt, nt = (full + kTile - 1) / kTile;
+        if (p_local < nt) {
+            const bool known = (unsigned)p_id < (unsigned)c.blocks;
+            const int id = known ? p_id : 0;
+            if (!known) refuse(a.status);
+            const unsigned at = smem_u32(&s_scale[warp][stage][0]);
+            if (lane < 4) {
+                // (lanes 0 and 1: k of the halves, 2 and 3: v of the halves; lane & 1 is the half whose number the lane holds)
+                if (known) cp_async_scale(at + lane * 4, (lane < 2 ? c.k_scale : c.v_scale) + id);
+                else sts_u32(at + lane * 4, 0x7fffffffu);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int token = p_local * kTile + u * 16;
+                const bool on = token < full;
+                const size_t from = ((size_t)__shfl_sync(0xffffffffu, id, u) * bt + token % bt) * D;
+                const unsigned char* const k = static_cast<const unsigned char*>(c.k_codes) + from + lane * 16;
+                const unsigned char* const v = static_cast<const unsigned char*>(c.v_codes) + from + lane * 16;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const int p = i * 32 + lane, r = p / CH, ch = p % CH;
+                    const unsigned to = dst + (unsigned)(ch * kTile + ((u * 16 + r) ^ (ch & 7))) * 16;
+                    cp_async_16_if(on, to, k + i * 512);
+                    cp_async_16_if(on, to + kTile * D, v + i * 512);
+                }
+            }
+        } else {
+            const int r0 = (p_local - nt) * 16;
+            const size_t from = ((size_t)p_stream * bt + r0) * D;
+            const __half* const k = static_cast<const __half*>(c.k_tail) + from + lane * 8;
+            const __half* const v = static_cast<const __half*>(c.v_tail) + from + lane * 8;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const int p = i * 32 + lane, r = p / (D / 8), ch = p % (D / 8);
+                const unsigned to = dst + (unsigned)(ch * 16 + (r ^ (ch & 7))) * 16;
+                const bool on = full + r0 + r < p_n;
+                cp_async_16_if(on, to, k + i * 256);
+                cp_async_16_if(on, to + kTile * D, v + i * 256);
+            }
+        }
+    };
+    look_up();
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) {
+        copy(i);
+        cp_async_commit();
+        look_up();
+    }
+
+    // ---- segment after segment
+    int stage = 0, tile = t0 + warp;
+    int seg = seg0, begin = begin0, n = n0;
+    while (begin < t1) {
+        const int tiles = tiles_of(n, bt), end = begin + tiles;
+        if (tiles == 0) {
+            ++seg;
+            n = length_of(seg / a.row_groups);
+            continue;
+        }
+        const int stream = seg / a.row_groups, row0 = seg % a.row_groups * ROWS;
+        const int b = stream / c.kv_heads, h = stream % c.kv_heads;
+        // queries: column g of set s is row row0 + 8s + g (with four rows twice the same four); a lane's dimensions of a chunk of 16
+        // are 4cc .. 4cc + 3, as its bytes of the codes are
+        unsigned qf[NC][CH][2];
+        int lim[NC][2];                       // tokens that the rows of this lane's columns see
+#pragma unroll
+        for (int s = 0; s < NC; ++s) {
+            const int r = row0 + s * 8 + (ROWS == 4 ? g & 3 : g);
+            const int i = r / a.group;
+            const __half* const q = a.q + (long long)b * a.q_batch + (long long)i * a.q_token + ((long long)h * a.group + (r - i * a.group)) * D + 4 * cc;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                uint2 v = make_uint2(0u, 0u);
+                if (r < a.rows) v = *reinterpret_cast<const uint2*>(q + j * 16);
+                qf[s][j][0] = v.x;
+                qf[s][j][1] = v.y;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int rc = row0 + s * 8 + (ROWS == 4 ? (2 * cc + e) & 3 : 2 * cc + e);
+                lim[s][e] = rc < a.rows ? n - a.queries + 1 + rc / a.group : n;
+            }
+        }
+        const int least = n - a.queries + 1;  // what all rows see
+        const int full = n / bt * bt, nt = (full + kTile - 1) / kTile;
+        float o[CH][NC][4];
+        float M[NC][2], l[NC][2];
+#pragma unroll
+        for (int s = 0; s < NC; ++s) {
+            M[s][0] = M[s][1] = -INFINITY;
+            l[s][0] = l[s][1] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < CH; ++d) o[d][s][0] = o[d][s][1] = o[d][s][2] = o[d][s][3] = 0.0f;
+        }
+        const int stop = min(end, t1);
+        for (; tile < stop; tile += NW) {
+            cp_async_wait<STAGES - 2>();
+            __syncwarp();
+            {
+                const int ahead = stage == 0 ? STAGES - 1 : stage - 1;
+                copy(ahead);
+                cp_async_commit();
+                look_up();
+            }
+            const unsigned at = ring + stage * S::kTileBytes;
+            const int local = tile - begin;
+            const bool codes = local < nt;
+            const int token0 = codes ? local * kTile : full + (local - nt) * 16;
+            float x[NC][2][4];                // scores: half u, (token g, column 2cc), (g, 2cc+1), (g+8, 2cc), (g+8, 2cc+1)
+            float ks[2] = {1.0f, 1.0f}, vs[2] = {1.0f, 1.0f};
+#pragma unroll
+            for (int s = 0; s < NC; ++s)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) x[s][u][0] = x[s][u][1] = x[s][u][2] = x[s][u][3] = 0.0f;
+            if (codes) {
+                const float4 sc = *reinterpret_cast<const float4*>(&s_scale[warp][stage][0]);
+                ks[0] = sc.x, vs[0] = sc.z;
+                if (token0 + 16 < full) ks[1] = sc.y, vs[1] = sc.w;
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    unsigned r[4], f[4][2];
+                    ldsm_x4(at + (unsigned)(j * kTile + (lane ^ (j & 7))) * 16, r);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) widen<FMT, false>(r[m], f[m][0], f[m][1]);
+#pragma unroll
+                    for (int s = 0; s < NC; ++s) {
+                        mma_16816(x[s][0], f[0][0], f[1][0], f[0][1], f[1][1], qf[s][j][0], qf[s][j][1]);
+                        mma_16816(x[s][1], f[2][0], f[3][0], f[2][1], f[3][1], qf[s][j][0], qf[s][j][1]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    const int ch = 2 * j + (cc >> 1);
+                    const uint2 r0 = lds_v2(at + (unsigned)(ch * 16 + (g ^ (ch & 7))) * 16 + (cc & 1) * 8);
+                    const uint2 r1 = lds_v2(at + (unsigned)(ch * 16 + ((g + 8) ^ (ch & 7))) * 16 + (cc & 1) * 8);
+#pragma unroll
+                    for (int s = 0; s < NC; ++s) mma_16816(x[s][0], r0.x, r1.x, r0.y, r1.y, qf[s][j][0], qf[s][j][1]);
+                }
+            }
+            // scores in powers of two; the v scale as 2^ve * vf, a scale of zero (or below the normal numbers) with ve = 0
+            float ve[2], vf[2], down[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const unsigned bits = __float_as_uint(vs[u]), ex = bits >> 23 & 0xffu;
+                const bool plain = ex != 0u && ex != 0xffu;
+                ve[u] = plain ? (float)((int)ex - 127) : 0.0f;
+                vf[u] = plain ? __uint_as_float((bits & 0x807fffffu) | 0x3f800000u) : vs[u];
+                down[u] = plain ? __uint_as_float((254u - ex) << 23) : 1.0f;      // 2^-ve
+                const float f = ks[u] * a.scale_log2;
+#pragma unroll
+                for (int s = 0; s < NC; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[s][u][e] *= f;
+            }
+            const int tokens = codes ? kTile : 16;
+            if (token0 + tokens > least || (codes && token0 + kTile > full) || !codes) {
+                // (a half tile behind the last full block counts for the next kind of tile)
+                const int seen = codes ? full : n;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int token = token0 + u * 16 + (e >> 1) * 8 + g;
+                        const bool in = token < seen && (codes || u == 0);
+#pragma unroll
+                        for (int s = 0; s < NC; ++s)
+                            if (!in || token >= lim[s][e & 1]) x[s][u][e] = -INFINITY;
+                    }
+            }
+            if (a.accumulate) {
+                float* const to = a.scores + (size_t)tile * (kTile * ROWS);
+                if (ROWS >= 8 || cc < 2) {
+#pragma unroll
+                    for (int s = 0; s < NC; ++s)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            *reinterpret_cast<float2*>(to + (u * 16 + g) * ROWS + s * 8 + 2 * cc) = make_float2(x[s][u][0], x[s][u][1]);
+                            *reinterpret_cast<float2*>(to + (u * 16 + g + 8) * ROWS + s * 8 + 2 * cc) = make_float2(x[s][u][2], x[s][u][3]);
+                        }
+                }
+            }
+            unsigned ph[NC][2][2], pl[NC][2][2];
+            float alpha[NC][2];
+            bool rescale = false;
+#pragma unroll
+            for (int s = 0; s < NC; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float m = fmaxf(fmaxf(x[s][0][e], x[s][0][e + 2]) + ve[0], fmaxf(x[s][1][e], x[s][1][e + 2]) + ve[1]);
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                    m = fmaxf(m, M[s][e]);
+                    alpha[s][e] = m == M[s][e] ? 1.0f : exp2_fast(M[s][e] - m);
+                    rescale = rescale || m != M[s][e];
+                    M[s][e] = m;
+                    l[s][e] *= alpha[s][e];
+                }
+            if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+                for (int d = 0; d < CH; ++d)
+#pragma unroll
+                    for (int s = 0; s < NC; ++s)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[d][s][e] *= alpha[s][e & 1];
+            }
+#pragma unroll
+            for (int s = 0; s < NC; ++s)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float m = M[s][e & 1];
+                        const float p = exp2_fast(x[s][u][e] + (ve[u] + kUp - (m == -INFINITY ? 0.0f : m)));
+                        l[s][e & 1] = fmaf(p, down[u], l[s][e & 1]);
+                        w[e] = x[s][u][e] == -INFINITY ? 0.0f : p * vf[u];   // (whatever the v scale of what is not seen)
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const unsigned hi = halves(w[2 * k], w[2 * k + 1]);
+                        const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                        const unsigned lo = halves(w[2 * k] - back.x, w[2 * k + 1] - back.y);
+                        if (ROWS == 4) {
+                            ph[s][u][k] = transposed(cc < 2 ? hi : lo);
+                        } else {
+                            ph[s][u][k] = transposed(hi);
+                            pl[s][u][k] = transposed(lo);
+                        }
+                    }
+                }
+            if (codes) {
+#pragma unroll
+                for (int d = 0; d < CH; ++d) {
+                    unsigned r[4], f[4][2];
+                    ldsm_x4_trans(at + kTile * D + (unsigned)(d * kTile + (lane ^ (d & 7))) * 16, r);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) widen<FMT, true>(r[m], f[m][0], f[m][1]);
+#pragma unroll
+                    for (int s = 0; s < NC; ++s) {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            mma_16816(o[d][s], f[2 * u][0], f[2 * u][1], f[2 * u + 1][0], f[2 * u + 1][1], ph[s][u][0], ph[s][u][1]);
+                            if (ROWS > 4) mma_16816(o[d][s], f[2 * u][0], f[2 * u][1], f[2 * u + 1][0], f[2 * u + 1][1], pl[s][u][0], pl[s][u][1]);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < CH; ++d) {
+                    const int ch = 2 * d + (g >> 2);
+                    unsigned w[4];
+                    bool odd = false;             // values that are not finite: out of the product, and to the rows that see them
+                    auto word = [&](int token) { return lds_u32(at + kTile * D + (unsigned)(ch * 16 + (token ^ (ch & 7))) * 16 + (g & 3) * 4); };
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        w[k] = word(2 * cc + (k & 1) + (k >> 1) * 8);
+                        const bool o0 = (w[k] & 0x7c00u) == 0x7c00u, o1 = (w[k] & 0x7c000000u) == 0x7c000000u;
+                        odd = odd || o0 || o1;
+                        w[k] &= (o0 ? 0u : 0xffffu) | (o1 ? 0u : 0xffff0000u);
+                    }
+                    const unsigned a0 = __byte_perm(w[0], w[1], 0x5410), a1 = __byte_perm(w[0], w[1], 0x7632);
+                    const unsigned a2 = __byte_perm(w[2], w[3], 0x5410), a3 = __byte_perm(w[2], w[3], 0x7632);
+#pragma unroll
+                    for (int s = 0; s < NC; ++s) {
+                        mma_16816(o[d][s], a0, a1, a2, a3, ph[s][0][0], ph[s][0][1]);
+                        if (ROWS > 4) mma_16816(o[d][s], a0, a1, a2, a3, pl[s][0][0], pl[s][0][1]);
+                    }
+                    if (__any_sync(0xffffffffu, odd)) {
+#pragma unroll 1
+                        for (int k = 0; k < 16 && token0 + k < n; ++k) {
+                            const unsigned v = word(k);
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+                            const bool o0 = (v & 0x7c00u) == 0x7c00u, o1 = (v & 0x7c000000u) == 0x7c000000u;
+#pragma unroll
+                            for (int s = 0; s < NC; ++s)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+                                    if (token0 + k < lim[s][e]) {
+                                        if (o0) o[d][s][e] += f.x;
+                                        if (o1) o[d][s][e + 2] += f.y;
+                                    }
+                        }
+                    }
+                }
+            }
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+        }
+
+        // ---- the warps' sums: to the CTA's largest M, then by way of shared memory, half the warps at a time
+#pragma unroll
+        for (int s = 0; s < NC; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                l[s][e] += __shfl_xor_sync(0xffffffffu, l[s][e], 4);
+                l[s][e] += __shfl_xor_sync(0xffffffffu, l[s][e], 8);
+                l[s][e] += __shfl_xor_sync(0xffffffffu, l[s][e], 16);
+                const int r = s * 8 + 2 * cc + e;
+                if (g == 0 && r < ROWS) s_ml[warp][r] = make_float2(M[s][e], l[s][e]);
+            }
+        if (ROWS == 4) {                      // the columns of what 16 bits did not hold
+#pragma unroll
+            for (int d = 0; d < CH; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][0][e] += __shfl_xor_sync(0xffffffffu, o[d][0][e], 2);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < NC; ++s) {
+            float f[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = s * 8 + 2 * cc + e;
+                float m = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) m = fmaxf(m, s_ml[w][r % ROWS].x);
+                f[e] = M[s][e] == m ? 1.0f : exp2_fast(M[s][e] - m);
+            }
+#pragma unroll
+            for (int d = 0; d < CH; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][s][e] *= f[e & 1];
+        }
+        const bool writes = ROWS >= 8 || cc < 2;
+        auto put = [&](float(*to)[S::kStride], bool add) {
+            if (!writes) return;
+#pragma unroll
+            for (int s = 0; s < NC; ++s)
+#pragma unroll
+                for (int d = 0; d < CH; ++d)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float2* const p = reinterpret_cast<float2*>(&to[s * 8 + 2 * cc + e][d * 16 + 2 * g]);
+                        float2 v = make_float2(o[d][s][e], o[d][s][e + 2]);
+                        if (add) {
+                            const float2 w = *p;
+                            v.x += w.x;
+                            v.y += w.y;
+                        }
+                        *p = v;
+                    }
+        };
+        if (warp >= NW / 2) put(s_o[warp - NW / 2], false);
+        __syncthreads();
+        if (warp < NW / 2) put(s_o[warp], true);
+        __syncthreads();
+        const bool whole = begin >= t0 && end <= t1;
+        const size_t part = (size_t)cta + seg;
+        for (int i = tid; i < ROWS * (D / 4); i += NW * 32) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4;
+            if (row0 + r >= a.rows) continue;
+            float m = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) m = fmaxf(m, s_ml[w][r].x);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float2 v = s_ml[w][r];
+                sum += v.x == m ? v.y : v.y * exp2_fast(v.x - m);
+            }
+            float4 v = *reinterpret_cast<const float4*>(&s_o[0][r][d]);
+#pragma unroll
+            for (int w = 1; w < NW / 2; ++w) {
+                const float4 k = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
+                v.x += k.x, v.y += k.y, v.z += k.z, v.w += k.w;
+            }
+            if (!whole) *reinterpret_cast<float4*>(a.o + (part * ROWS + r) * D + d) = v;
+            if ((!whole || a.accumulate) && d == 0) a.ml[part * ROWS + r] = make_float2(m, sum);
+            if (whole) {
+                const int rr = row0 + r, qi = rr / a.group;
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;           // (a row that sees nothing: zeros)
+                __half* const to = a.out + (long long)b * a.out_batch + (long long)qi * a.out_token + ((long long)h * a.group + (rr - qi * a.group)) * D + d;
+                const uint2 hv = make_uint2(halves(v.x * inv, v.y * inv), halves(v.z * inv, v.w * inv));
+                *reinterpret_cast<uint2*>(to) = hv;
+            }
+        }
+        __syncthreads();
+        begin = end;
+        ++seg;
+        n = begin < t1 ? length_of(seg / a.row_groups) : 0;
+    }
+    cp_async_wait<0>();
+}
+
+// ---------------------------------------------------------------- the parts together
+
+// The (M, l) of a row over the CTAs that had part of its segment, by the lanes of a warp; and the CTAs.
+__device__ __forceinline__ float2 joined(const float2* ml, int rows, int seg, int r, int c0, int c1, int lane)
+{
+    float m = -INFINITY, l = 0.0f;
+    for (int i = c0 + lane; i <= c1; i += 32) {
+        const float2 v = ml[((size_t)i + seg) * rows + r];
+        const float top = fmaxf(m, v.x);
+        l = (m == top ? l : l * exp2_fast(m - top)) + (v.x == top ? v.y : v.y * exp2_fast(v.x - top));
+        m = top;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float om = __shfl_xor_sync(0xffffffffu, m, o), ol = __shfl_xor_sync(0xffffffffu, l, o);
+        const float top = fmaxf(m, om);
+        // (the two lanes of a pair add the same two values)
+        l = (m == top ? l : l * exp2_fast(m - top)) + (om == top ? ol : ol * exp2_fast(om - top));
+        m = top;
+    }
+    return make_float2(m, l);
+}
+
+constexpr int kJoinWarps = 4;
+
+// CTAs below `rows_ctas`: one row of one segment each, its parts' sums added in the order of the CTAs (by four warps, then the
+// four).  The others: an equal part of all tiles each, a lane per token.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(const AttnArgs a, int streams, int rows_ctas, int parts, int warps)
+{
+    __shared__ float s_o[kJoinWarps][D];
+    __shared__ float2 s_ml[64];
+    const spqt_kv_cache& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bt = c.block_tokens;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int segments = streams * a.row_groups, total = (int)ld_global_u32(a.begin + segments);
+    const int ctas = working_ctas(total, warps, parts);
+    if ((int)blockIdx.x < rows_ctas) {
+        const int rr = blockIdx.x % a.rows, stream = blockIdx.x / a.rows, rg = rr / ROWS, r = rr % ROWS, seg = stream * a.row_groups + rg;
+        const int b = stream / c.kv_heads, h = stream % c.kv_heads, qi = rr / a.group;
+        const int begin = (int)ld_global_u32(a.begin + seg);   // (of an empty stream: of no meaning)
+        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, bt);
+        __half* const out = a.out + (long long)b * a.out_batch + (long long)qi * a.out_token + ((long long)h * a.group + (rr - qi * a.group)) * D;
+        if (tiles == 0) {
+            for (int d = tid * 2; d < D; d += kJoinWarps * 64) *reinterpret_cast<unsigned*>(out + d) = 0u;
+            return;
+        }
+        const int c0 = owner_of(begin, total, ctas), c1 = owner_of(begin + tiles - 1, total, ctas);
+        if (c0 == c1) return;                 // finished where it was computed
+        const float2 ml = joined(a.ml, ROWS, seg, r, c0, c1, lane);
+        constexpr int V = (D + 127) / 128;
+        float4 sum[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int i = c0 + warp; i <= c1; i += kJoinWarps) {
+            const size_t at = ((size_t)i + seg) * ROWS + r;
+            const float m = a.ml[at].x;
+            const float f = m == ml.x ? 1.0f : exp2_fast(m - ml.x);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int d = v * 128 + lane * 4;
+                if (d < D) {
+                    const float4 k = *reinterpret_cast<const float4*>(a.o + at * D + d);
+                    sum[v].x = fmaf(k.x, f, sum[v].x), sum[v].y = fmaf(k.y, f, sum[v].y);
+                    sum[v].z = fmaf(k.z, f, sum[v].z), sum[v].w = fmaf(k.w, f, sum[v].w);
+                }
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v * 128 + lane * 4 < D) *reinterpret_cast<float4*>(&s_o[warp][v * 128 + lane * 4]) = sum[v];
+        __syncthreads();
+        const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
+        for (int d = tid; d < D; d += kJoinWarps * 32) {
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kJoinWarps; ++w) v += s_o[w][d];
+            out[d] = __float2half_rn(v * inv);
+        }
+        return;
+    }
+    // weights: tiles of the streams' first row groups, numbered end to end
+    const int all = total / a.row_groups, me = blockIdx.x - rows_ctas, them = gridDim.x - rows_ctas;
+    const int t0 = (int)((long long)all * me / them), t1 = (int)((long long)all * (me + 1) / them);
+    if (t0 >= t1) return;
+    // the stream of t0: the last that begins there or before (streams without tokens begin where the next one does)
+    int stream = 0;
+    for (int left = streams; left > 1;) {                // (the lanes of a warp look at 32 places at a time)
+        const int step = (left + 31) / 32, at = lane * step;
+        const unsigned mask = __ballot_sync(0xffffffffu, at < left && (int)ld_global_u32(a.begin + (size_t)(stream + min(at, left - 1)) * a.row_groups) / a.row_groups <= t0);
+        const int k = (31 - __clz(mask)) * step;         // (the first place always counts)
+        stream += k;
+        left = min(step, left - k);
+    }
+    for (int t = t0; t < t1;) {
+        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, bt);
+        if (tiles == 0) {
+            ++stream;
+            continue;
+        }
+        const int seg = stream * a.row_groups, begin = (int)ld_global_u32(a.begin + seg), first = begin / a.row_groups;
+        const int stop = min(t1, first + tiles), full = n / bt * bt, nt = (full + kTile - 1) / kTile;
+        const int32_t* const row = c.table + (size_t)stream * c.table_width;
+        for (int rb = 0; rb < a.rows; rb += 64) {      // 64 rows at a time
+            const int rows = min(64, a.rows - rb);
+            __syncthreads();
+            for (int r = warp; r < rows; r += kJoinWarps) {
+                const int rg = (rb + r) / ROWS, sg = seg + rg, bg = begin + rg * tiles;
+                const float2 v = joined(a.ml, ROWS, sg, (rb + r) % ROWS, owner_of(bg, total, ctas), owner_of(bg + tiles - 1, total, ctas), lane);
+                if (lane == 0) s_ml[r] = make_float2(v.x == -INFINITY ? 0.0f : v.x - kUp, v.y == 0.0f ? 0.0f : 1.0f / v.y);
+            }
+            __syncthreads();
+            for (int x = t + warp; x < stop; x += kJoinWarps) {
+                const int local = x - first;
+                const bool codes = local < nt;
+                const int token = (codes ? local * kTile : full + (local - nt) * 16) + lane;
+                if (token >= (codes ? full : n) || (!codes && lane >= 16)) continue;
+                const unsigned block = (unsigned)row[token / bt];
+                if (block >= (unsigned)c.blocks) {
+                    refuse(a.status);
+                    continue;
+                }
+                float sum = 0.0f;
+                for (int r = 0; r < rows; r += 4) {
+                    const int rg = (rb + r) / ROWS;
+                    const float4 s = *reinterpret_cast<const float4*>(a.scores + ((size_t)(begin + rg * tiles + local) * kTile + lane) * ROWS + (rb + r) % ROWS);
+                    const float e[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (r + k < rows) sum = fmaf(exp2_fast(e[k] - s_ml[r + k].x), s_ml[r + k].y, sum);
+                }
+                c.weight[(size_t)block * bt + token % bt] += sum;
+            }
+        }
+        t = stop;
+        ++stream;
+    }
+}
+
+// ---------------------------------------------------------------- host
+
+inline int rows_of(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+
+struct AttnWorkspace {
+    size_t begin, ml, o, scores, bytes;
+};
+
+// false where the tiles' numbers would pass 31 bits
+inline bool attention_workspace(const spqt_kv_cache& c, int group, int queries, AttnWorkspace* w)
+{
+    const int rows = group * queries, R = rows_of(rows), groups = (rows + R - 1) / R;
+    const long long streams = (long long)c.batch * c.kv_heads, segments = streams * groups;
+    const long long tiles = segments * (((long long)c.table_width * c.block_tokens + kTile - 1) / kTile + 8);
+    if (segments > kMaxStreams || tiles > 0x7fffffffLL) return false;
+    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    size_t at = kKvHeader;
+    w->begin = at, at += up(((size_t)segments + 1) * 4);
+    const size_t parts = (size_t)(kMaxAttnCtas + segments);
+    w->ml = at, at += up(parts * R * 8);
+    w->o = at, at += up(parts * R * c.head_dim * 4);
+    w->scores = at;
+    if (c.weight) at += up((size_t)tiles * kTile * R * 4);
+    const size_t lengths = kKvHeader + kv_lengths_bytes(c);
+    w->bytes = at > lengths ? at : lengths;
+    return true;
+}
+
+template <int FMT, int D, int ROWS>
+cudaError_t launch_attention(const AttnArgs& a, cudaStream_t s)
+{
+    using S = AttnShape<D, ROWS>;
+    constexpr size_t smem = (size_t)S::kWarps * S::kStages * S::kTileBytes;
+    static thread_local int allowed_dev = -1;
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    if (allowed_dev != dev) {
+        err = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err != cudaSuccess) return err;
+        allowed_dev = dev;
+    }
+    const int sms = sm_count();
+    if (sms <= 0) return cudaErrorInvalidDevice;
+    const int parts = sms < kMaxAttnCtas ? sms : kMaxAttnCtas, streams = a.c.batch * a.c.kv_heads;
+    err = launch_overlapping(kv_attention_kernel<FMT, D, ROWS>, dim3(parts), S::kWarps * 32, smem, s, a, streams);
+    if (err != cudaSuccess) return err;
+    const int rows_ctas = streams * a.rows;
+    return launch_overlapping(kv_attention_join_kernel<D, ROWS>, dim3(rows_ctas + (a.accumulate ? 4 * sms : 0)), kJoinWarps * 32, 0, s, a, streams, rows_ctas,
+                              parts, S::kWarps);
+}
+
+template <int FMT, int D>
+cudaError_t launch_rows(const AttnArgs& a, cudaStream_t s)
+{
+    const int r = rows_of(a.rows);
+    return r == 4 ? launch_attention<FMT, D, 4>(a, s) : r == 8 ? launch_attention<FMT, D, 8>(a, s) : launch_attention<FMT, D, 16>(a, s);
+}
+
+template <int FMT>
+cudaError_t launch_dim(const AttnArgs& a, cudaStream_t s)
+{
+    switch (a.c.head_dim) {
+        case 64: return launch_rows<FMT, 64>(a, s);
+        case 96: return launch_rows<FMT, 96>(a, s);
+        case 128: return launch_rows<FMT, 128>(a, s);
+        default: return launch_rows<FMT, 256>(a, s);
+    }
+}
+
+static spqt_status check_rows(const spqt_kv_cache* cache, int q_heads, int queries, AttnWorkspace* w)
+{
+    spqt_status st = check_cache(cache);
+    if (st != SPQT_OK) return st;
+    if (q_heads <= 0 || queries <= 0) return SPQT_ERR_INVALID_ARG;
+    if (q_heads % cache->kv_heads || q_heads / cache->kv_heads > 64 || queries > 16) return SPQT_ERR_UNSUPPORTED;
+    return attention_workspace(*cache, q_heads / cache->kv_heads, queries, w) ? SPQT_OK : SPQT_ERR_UNSUPPORTED;
+}
+
+}  // namespace spqt
+
+extern "C" {
+
+spqt_status spqt_kv_workspace(const spqt_kv_cache* cache, int q_heads, int queries, size_t* bytes)
+{
+    spqt::AttnWorkspace w;
+    if (!bytes) return SPQT_ERR_INVALID_ARG;
+    spqt_status st = spqt::check_rows(cache, q_heads, queries, &w);
+    if (st != SPQT_OK) return st;
+    // (fewer queries may take the rows in other groups)
+    size_t most = w.bytes;
+    for (int q = 1; q < queries; ++q) {
+        st = spqt::check_rows(cache, q_heads, q, &w);
+        if (st == SPQT_OK && w.bytes > most) most = w.bytes;
+    }
+    *bytes = most;
+    return SPQT_OK;
+}
+
+spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long long q_batch_stride, long long q_token_stride, int q_heads, int queries,
+                              float scale, int accumulate, void* out, long long out_batch_stride, long long out_token_stride, void* workspace,
+                              size_t workspace_bytes, void* stream)
+{
+    using namespace spqt;
+    AttnWorkspace w;
+    spqt_status st = check_rows(cache, q_heads, queries, &w);
+    if (st != SPQT_OK) return st;
+    if (!q || !out || (accumulate && !cache->weight) || q_batch_stride < 0 || q_token_stride < 0 || out_batch_stride < 0 || out_token_stride < 0)
+        return SPQT_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || q_batch_stride % 8 || q_token_stride % 8 || out_batch_stride % 8 || out_token_stride % 8) return SPQT_ERR_ALIGNMENT;
+    st = check_kv_workspace(workspace, workspace_bytes, accumulate ? w.bytes : w.scores);
+    if (st != SPQT_OK) return st;
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    const int group = q_heads / cache->kv_heads, rows = group * queries, R = rows_of(rows);
+    const AttnArgs a = {*cache, static_cast<const __half*>(q), q_batch_stride, q_token_stride, static_cast<__half*>(out), out_batch_stride, out_token_stride,
+                        group, queries, rows, (rows + R - 1) / R, accumulate ? 1 : 0, scale * 1.4426950408889634f, static_cast<int*>(status_word(workspace)),
+                        reinterpret_cast<int*>(ws + w.begin), reinterpret_cast<float2*>(ws + w.ml), reinterpret_cast<float*>(ws + w.o),
+                        reinterpret_cast<float*>(ws + w.scores)};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return launched(cache->format == SPQT_KV_INT8 ? launch_dim<SPQT_KV_INT8>(a, s) : launch_dim<SPQT_KV_E4M3>(a, s));
+}
+
+}  // extern "C"

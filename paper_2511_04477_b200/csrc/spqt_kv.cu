@@ -1,0 +1,497 @@
+// The 8-bit cache but for the attention over it: new tokens (with the rounding of blocks that become full), the cache as fp16,
+// and the eviction of blocks.
+#include <cuda_fp8.h>
+
+#include "spqt_common.cuh"
+#include "spqt_gemv_device.cuh"
+#include "spqt_kv.cuh"
+
+namespace spqt {
+
+// ---------------------------------------------------------------- eight values to codes and back
+
+// x / s rounded to the nearest whole number, ties to even, in one rounding: q is the whole number next to x * (1/s), which is off
+// by one at most where x/s is within 2^-16 of a tie; x - q*s is exact (|q| < 2^7 times 24 bits of s, of which x is a neighbour),
+// and says on which side of the tie x/s lies.
+__device__ __forceinline__ unsigned to_int8(float x, float s, float inv)
+{
+    constexpr float kMagic = 12582912.0f;   // 1.5 * 2^23: its sum's last bits are the whole number
+    float t = fmaf(x, inv, kMagic);
+    const float r = fmaf(-(t - kMagic), s, x);
+    const float a = 2.0f * fabsf(r);
+    if (a >= s && (a > s || (__float_as_uint(t) & 1u))) t += copysignf(1.0f, r);
+    return __float_as_uint(t) & 0xffu;
+}
+
+// x / s in fp32 with its last bit set where the quotient is not exact: a second rounding to few bits then gives what one rounding
+// of the exact quotient gives.  q is x/s to the last place or next to it, and the sign of x - q*s (exact in an FMA) says between
+// which two neighbours x/s lies.
+__device__ __forceinline__ float quotient_to_odd(float x, float s, float inv)
+{
+    const float q0 = x * inv;
+    const float q = fmaf(fmaf(-q0, s, x), inv, q0);
+    const float r = fmaf(-q, s, x);
+    const unsigned bits = __float_as_uint(q);
+    const unsigned over = (__float_as_uint(r) ^ bits) >> 31;     // |q| > |x/s|
+    return __uint_as_float((r == 0.0f ? bits : (bits - over) | 1u) | (__float_as_uint(x) & 0x80000000u));   // (-0 / s is -0)
+}
+
+template <int FMT>
+__device__ __forceinline__ uint2 to_codes(const uint4& h, float s, float inv)
+{
+    const __half2* p = reinterpret_cast<const __half2*>(&h);
+    unsigned w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(p[i]);
+        unsigned pair;
+        if (FMT == SPQT_KV_INT8)
+            pair = to_int8(f.x, s, inv) | to_int8(f.y, s, inv) << 8;
+        else
+            pair = __nv_cvt_float2_to_fp8x2(make_float2(quotient_to_odd(f.x, s, inv), quotient_to_odd(f.y, s, inv)), __NV_SATFINITE, __NV_E4M3);
+        w[i >> 1] |= pair << (16 * (i & 1));
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+template <int FMT>
+__device__ __forceinline__ uint4 from_codes(const uint2& w, float s)
+{
+    uint4 h;
+    __half2* p = reinterpret_cast<__half2*>(&h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned pair = (i < 2 ? w.x : w.y) >> (16 * (i & 1)) & 0xffffu;
+        float2 f;
+        if (FMT == SPQT_KV_INT8)
+            f = make_float2((float)(signed char)(pair & 0xffu), (float)(signed char)(pair >> 8));
+        else
+            f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
+        p[i] = __floats2half2_rn(f.x * s, f.y * s);
+    }
+    return h;
+}
+
+// ---------------------------------------------------------------- new tokens
+
+// A CTA works on one touched block of one stream: its first half of threads on the keys, the second on the values, a thread on up
+// to PPT 16-byte pieces of the block's rows, which stay in registers between the maximum and the rounding, so that every row is
+// read once.  Memory is what bounds a prompt: 4 bytes read and 2 written per value pair; heads of a block of tokens are neighbours
+// in the grid, since their rows are neighbours in memory.
+struct AppendArgs {
+    spqt_kv_cache c;
+    const __half *k, *v;
+    int tokens;
+    long long batch_stride, token_stride;
+    const int32_t* counts;
+    int32_t* length_out;
+    int* status;
+};
+
+template <int FMT, int D, int PPT>
+__global__ void __launch_bounds__(1024) kv_append_kernel(const AppendArgs a)
+{
+    __shared__ unsigned s_max[32];
+    const spqt_kv_cache& c = a.c;
+    const int tid = threadIdx.x, half = blockDim.x >> 1, warp = tid >> 5;
+    const int h = blockIdx.x % c.kv_heads, j = blockIdx.x / c.kv_heads, b = blockIdx.y;
+    const int stream = b * c.kv_heads + h, bt = c.block_tokens;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    const int held = (int)ld_global_u32(c.length + stream);
+    int count = a.counts ? (int)ld_global_u32(a.counts + b) : a.tokens;
+    const int n = length_or_none(held, c, a.status);
+    if (count < 0 || count > a.tokens) {
+        refuse(a.status);
+        count = 0;
+    }
+    const int first = n / bt, before = n % bt;
+    const long long end = (long long)n + count;
+    const int total = before + count;               // rows from the beginning of block `first` on
+    const int touched = (total + bt - 1) / bt;
+    bool fine = held == n && end <= (long long)c.table_width * bt;
+    const int32_t* const row = c.table + (size_t)stream * c.table_width + first;
+    if (count > 0) {                                // every CTA of the stream comes to the same verdict
+        bool bad = false;
+        if (fine)
+            for (int i = tid; i < touched; i += blockDim.x) bad = bad || (unsigned)row[i] >= (unsigned)c.blocks;
+        fine = !__syncthreads_or(bad) && fine;
+        if (!fine) refuse(a.status);
+    }
+    if (!fine || count == 0) {
+        if (j == 0 && tid == 0 && a.length_out) a.length_out[stream] = held;
+        return;
+    }
+    if (j >= touched) return;
+    const size_t block = (size_t)row[j];
+
+    if (c.weight) {
+        const int from = j == 0 ? before : 0, to = min(bt, total - j * bt);
+        for (int i = from + tid; i < to; i += blockDim.x) c.weight[block * bt + i] = 0.0f;
+    }
+    const bool values = tid >= half;
+    const int t = values ? tid - half : tid;
+    const int closed = total / bt;
+    const __half* const fresh = (values ? a.v : a.k) + (long long)b * a.batch_stride + (long long)h * D;
+    __half* const tail = static_cast<__half*>(values ? c.v_tail : c.k_tail) + (size_t)stream * bt * D;
+    constexpr int kRow = D / 8;                     // pieces of a row
+    if (j < closed) {
+        uint4 x[PPT];
+        unsigned top = 0u;
+        const int pieces = bt * kRow;
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+            const int p = i * half + t, r = p / kRow, at = j * bt + r - before;
+            const __half* src = at < 0 ? tail + r * D : fresh + (long long)at * a.token_stride;
+            x[i] = ld_global_v4_if(p < pieces, src + p % kRow * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+            // (magnitudes of fp16 in the order of their bits, not-a-number above infinity)
+            top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu)));
+        }
+        top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+        if ((tid & 31) == 0) s_max[warp] = top;
+        __syncthreads();
+        const int w0 = values ? half >> 5 : 0;
+        for (int w = 0; w < half >> 5; ++w) top = max(top, s_max[w0 + w]);
+        const bool poisoned = top >= 0x7c00u;
+        const float amax = __half2float(__ushort_as_half((unsigned short)top));
+        const float s = poisoned ? __int_as_float(0x7fffffff) : __fdiv_rn(amax, FMT == SPQT_KV_INT8 ? 127.0f : 448.0f);
+        const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+        uint2* const dst = reinterpret_cast<uint2*>(static_cast<unsigned char*>(values ? c.v_codes : c.k_codes) + block * bt * D);
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+            const int p = i * half + t;
+            if (p < pieces) dst[p] = poisoned ? make_uint2(0u, 0u) : to_codes<FMT>(x[i], s, inv);
+        }
+        if (t == 0) (values ? c.v_scale : c.k_scale)[block] = s;
+    }
+    if (j != 0) return;
+    // The CTA that has read the tail is the one that writes it, behind its last read.
+    __syncthreads();
+    const int base = closed * bt;                   // the first row of the block that stays open
+    const int from = closed > 0 ? 0 : before, rows = total - base;
+    for (int p = from * kRow + t; p < rows * kRow; p += half)
+        *reinterpret_cast<uint4*>(tail + p * 8) = ld_global_v4(fresh + (long long)(base + p / kRow - before) * a.token_stride + p % kRow * 8);
+    if (tid == 0 && a.length_out) a.length_out[stream] = (int)end;
+}
+
+// Lengths in place of the old ones, behind a kernel several of whose CTAs read the old one.
+__global__ void kv_lengths_kernel(const int32_t* from, int32_t* to, int n)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < n) to[i] = from[i];
+}
+
+template <int FMT, int D>
+cudaError_t launch_append(const AppendArgs& a, cudaStream_t s)
+{
+    const int bt = a.c.block_tokens, pieces = bt * D / 8;
+    const int touched = (int)(((long long)a.tokens + 2 * bt - 2) / bt);
+    const dim3 grid((unsigned)(touched * a.c.kv_heads), (unsigned)a.c.batch);
+    if (pieces <= 2048) {
+        const int half = (pieces / 4 + 31) / 32 * 32;
+        return launch_overlapping(kv_append_kernel<FMT, D, 4>, grid, 2 * half, 0, s, a);
+    }
+    return launch_overlapping(kv_append_kernel<FMT, D, 8>, grid, 1024, 0, s, a);
+}
+
+// ---------------------------------------------------------------- the cache as fp16
+
+struct ReadArgs {
+    spqt_kv_cache c;
+    const int32_t* length;
+    __half *k, *v;
+    int tokens;
+    long long batch_stride, token_stride, head_stride;
+    int* status;
+};
+
+constexpr int kReadTokens = 16;   // of a CTA: a part of one block of every stream of a sequence
+
+// Pieces of eight values, those of a row and then the heads of a token side by side, as the output has them.
+template <int FMT, int D>
+__global__ void __launch_bounds__(256) kv_read_kernel(const ReadArgs a)
+{
+    const spqt_kv_cache& c = a.c;
+    constexpr int kRow = D / 8;
+    const int t0 = blockIdx.x * kReadTokens, b = blockIdx.y, bt = c.block_tokens;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int per_token = c.kv_heads * kRow;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < kReadTokens * per_token; i += 256) {
+        const int t = t0 + i / per_token, rest = i % per_token, h = rest / kRow, p = rest % kRow;
+        const int stream = b * c.kv_heads + h;
+        const int n = length_or_none(a.length[stream], c, a.status);
+        if (t >= n || t >= a.tokens) continue;
+        uint4 k, v;
+        const int j = t / bt, r = t % bt;
+        if (t < n / bt * bt) {
+            const unsigned block = (unsigned)c.table[(size_t)stream * c.table_width + j];
+            const bool known = block < (unsigned)c.blocks;
+            const size_t id = known ? block : 0u;
+            const size_t at = (id * bt + r) * D + p * 8;
+            float ks = c.k_scale[id], vs = c.v_scale[id];
+            if (!known) {
+                refuse(a.status);
+                ks = vs = __int_as_float(0x7fffffff);
+            }
+            k = from_codes<FMT>(*reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k_codes) + at), ks);
+            v = from_codes<FMT>(*reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v_codes) + at), vs);
+        } else {
+            const size_t at = ((size_t)stream * bt + r) * D + p * 8;
+            k = *reinterpret_cast<const uint4*>(static_cast<const __half*>(c.k_tail) + at);
+            v = *reinterpret_cast<const uint4*>(static_cast<const __half*>(c.v_tail) + at);
+        }
+        const long long to = (long long)b * a.batch_stride + (long long)t * a.token_stride + (long long)h * a.head_stride + p * 8;
+        *reinterpret_cast<uint4*>(a.k + to) = k;
+        *reinterpret_cast<uint4*>(a.v + to) = v;
+    }
+}
+
+// ---------------------------------------------------------------- eviction
+
+constexpr int kEvictThreads = 512, kEvictWarps = kEvictThreads / 32;
+
+struct EvictArgs {
+    spqt_kv_cache c;
+    int keep, first, recent;
+    int32_t *table_out, *length_out;
+    int* status;
+};
+
+// Whole numbers in the order of fp32 values, not-a-number above all, zeros of both signs alike.
+__device__ __forceinline__ unsigned ordered(float f)
+{
+    if (f != f) return 0xffffffffu;
+    const unsigned u = __float_as_uint(f + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// How many of the CTA's values are true, and how many are in threads before this one (in thread order).
+__device__ __forceinline__ int count_before(bool v, int* s_warps, int* all)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned mask = __ballot_sync(0xffffffffu, v);
+    __syncthreads();                        // (s_warps may still be read)
+    if (lane == 0) s_warps[warp] = __popc(mask);
+    __syncthreads();
+    const int mine = lane < kEvictWarps ? s_warps[lane] : 0;
+    *all = __reduce_add_sync(0xffffffffu, mine);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0) + __popc(mask & ((1u << lane) - 1u));
+}
+
+// One CTA per stream: the blocks' sums as ordered whole numbers in shared memory beside the row of the table; the m-th largest by
+// two bits a round; then one pass in order.  The weights are read once; the rest is latency.
+__global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs a)
+{
+    extern __shared__ unsigned s_dyn[];     // keys [table_width], then the row of the table [table_width]
+    __shared__ int s_count[16][3], s_warps[kEvictWarps];
+    const spqt_kv_cache& c = a.c;
+    const int stream = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int bt = c.block_tokens, width = c.table_width;
+    unsigned* const s_key = s_dyn;
+    int* const s_row = reinterpret_cast<int*>(s_dyn + width);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int held = (int)ld_global_u32(c.length + stream);
+    const int n = length_or_none(held, c, a.status);
+    const int32_t* const row = c.table + (size_t)stream * width;
+    int32_t* const row_out = (a.table_out ? a.table_out : c.table) + (size_t)stream * width;
+    int32_t* const length_out = (a.length_out ? a.length_out : c.length) + stream;
+    const int closed = n / bt;
+    if (closed <= a.keep) {
+        if (row_out != row)
+            for (int i = tid; i < width; i += kEvictThreads) row_out[i] = row[i];
+        if (tid == 0) *length_out = held;
+        return;
+    }
+    for (int i = tid; i < width; i += kEvictThreads) s_row[i] = row[i];
+    if (tid < 48) s_count[tid / 3][tid % 3] = 0;
+    __syncthreads();
+    // sums: bt / 4 lanes a block, four weights a lane, in fp64 (the order of the sum is then of no consequence to the rounded one
+    // but in one case of 2^29)
+    const int lanes = bt >> 2, at_once = 32 / lanes, sub = lane / lanes, l = lane % lanes;
+    constexpr int kU = 4;
+    for (int j0 = warp * at_once * kU; j0 < closed; j0 += kEvictWarps * at_once * kU) {
+        float4 w[kU];
+        bool known[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int j = j0 + u * at_once + sub;
+            const unsigned id = j < closed ? (unsigned)s_row[j] : 0u;
+            known[u] = id < (unsigned)c.blocks;
+            w[u] = j < closed && known[u] ? *reinterpret_cast<const float4*>(c.weight + (size_t)id * bt + 4 * l) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int j = j0 + u * at_once + sub;
+            double v = ((double)w[u].x + w[u].y) + ((double)w[u].z + w[u].w);
+            for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (l == 0 && j < closed) {
+                s_key[j] = known[u] ? ordered((float)v) : 0u;      // (what no block stands behind leaves first)
+                if (!known[u]) refuse(a.status);
+            }
+        }
+    }
+    __syncthreads();
+    // the m-th largest key among the blocks that are not protected
+    const int lo = a.first, hi = closed - a.recent, m = a.keep - a.first - a.recent;
+    unsigned key = 0u;                      // its bits so far
+    int above = 0;                          // keys above all that share these bits
+    if (m > 0) {
+        for (int round = 0; round < 16; ++round) {
+            const int shift = 30 - 2 * round;
+            const unsigned t1 = key | 1u << shift, t2 = key | 2u << shift, t3 = key | 3u << shift;
+            int c1 = 0, c2 = 0, c3 = 0;
+            for (int j = lo + tid; j < hi; j += kEvictThreads) {
+                const unsigned k = s_key[j];
+                c1 += k >= t1, c2 += k >= t2, c3 += k >= t3;
+            }
+            c1 = __reduce_add_sync(0xffffffffu, c1), c2 = __reduce_add_sync(0xffffffffu, c2), c3 = __reduce_add_sync(0xffffffffu, c3);
+            if (lane == 0) {
+                if (c1) atomicAdd(&s_count[round][0], c1);
+                if (c2) atomicAdd(&s_count[round][1], c2);
+                if (c3) atomicAdd(&s_count[round][2], c3);
+            }
+            __syncthreads();
+            const int a1 = s_count[round][0], a2 = s_count[round][1], a3 = s_count[round][2];
+            key = a3 >= m ? t3 : a2 >= m ? t2 : a1 >= m ? t1 : key;
+            if (a3 == m || a2 == m || a1 == m) break;   // these m and no other reach `key`
+        }
+        int more = 0;
+        for (int j = lo + tid; j < hi; j += kEvictThreads) more += s_key[j] > key;
+        more = __reduce_add_sync(0xffffffffu, more);
+        __syncthreads();
+        if (lane == 0) s_warps[warp] = more;
+        __syncthreads();
+        for (int w = 0; w < kEvictWarps; ++w) above += s_warps[w];
+    }
+    // in order: blocks that stay to the front, the open one, those that leave, the rest where it was
+    const int some = n % bt ? 1 : 0;
+    int equal = m - above, stay = 0, leave = a.keep + some;   // places: of the equal ones only the first `equal` stay
+    for (int j0 = 0; j0 < closed; j0 += kEvictThreads) {
+        const int j = j0 + tid;
+        const bool in = j >= lo && j < hi;
+        const unsigned k = in ? s_key[j] : 0u;
+        int all;
+        const bool same = in && m > 0 && k == key;
+        const int rank = count_before(same, s_warps, &all);
+        const bool keeps = j < closed && (!in || (m > 0 && (k > key || (same && rank < equal))));
+        equal -= all;
+        const int place = count_before(keeps, s_warps, &all);
+        if (j < closed) row_out[keeps ? stay + place : leave + tid - place] = s_row[j];
+        stay += all;
+        leave += min(kEvictThreads, closed - j0) - all;
+    }
+    if (some && tid == 0) row_out[a.keep] = s_row[closed];
+    if (row_out != row)
+        for (int i = closed + some + tid; i < width; i += kEvictThreads) row_out[i] = s_row[i];
+    if (tid == 0) *length_out = a.keep * bt + n % bt;
+}
+
+}  // namespace spqt
+
+// Calls `f` with the cache's format and row size as constants.
+#define SPQT_KV_DISPATCH(c, f)                                                            \
+    ((c).format == SPQT_KV_INT8 ? ((c).head_dim == 64    ? f(SPQT_KV_INT8, 64)            \
+                                   : (c).head_dim == 96  ? f(SPQT_KV_INT8, 96)            \
+                                   : (c).head_dim == 128 ? f(SPQT_KV_INT8, 128)           \
+                                                         : f(SPQT_KV_INT8, 256))          \
+                                : ((c).head_dim == 64    ? f(SPQT_KV_E4M3, 64)            \
+                                   : (c).head_dim == 96  ? f(SPQT_KV_E4M3, 96)            \
+                                   : (c).head_dim == 128 ? f(SPQT_KV_E4M3, 128)           \
+                                                         : f(SPQT_KV_E4M3, 256)))
+
+extern "C" {
+
+spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void* v, int tokens, long long batch_stride, long long token_stride,
+                           const int32_t* counts, int32_t* length_out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace spqt;
+    spqt_status st = check_cache(cache);
+    if (st != SPQT_OK) return st;
+    if (!k || !v || tokens < 1 || batch_stride < 0 || token_stride < 0) return SPQT_ERR_INVALID_ARG;
+    if (!aligned(k, 16) || !aligned(v, 16) || batch_stride % 8 || token_stride % 8 || !aligned(counts, 4) || !aligned(length_out, 4)) return SPQT_ERR_ALIGNMENT;
+    if (cache->batch > 65535 || tokens > (1 << 28) || ((long long)tokens + 2 * cache->block_tokens) / cache->block_tokens * cache->kv_heads >= 0x7fffffffLL)
+        return SPQT_ERR_UNSUPPORTED;
+    st = check_kv_workspace(workspace, workspace_bytes, kKvHeader + kv_lengths_bytes(*cache));
+    if (st != SPQT_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    AppendArgs a = {*cache, static_cast<const __half*>(k), static_cast<const __half*>(v), tokens, batch_stride, token_stride, counts,
+                    length_out ? length_out : cache->length, static_cast<int*>(status_word(workspace))};
+    // Lengths are written in place at once where one CTA per stream reads them (a single token); else by way of the workspace.
+    const bool indirect = a.length_out == cache->length && tokens > 1;
+    if (indirect) a.length_out = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + kKvHeader);
+#define SPQT_F(F, D) launch_append<F, D>(a, s)
+    cudaError_t err = SPQT_KV_DISPATCH(*cache, SPQT_F);
+#undef SPQT_F
+    if (err == cudaSuccess && indirect) {
+        const int n = cache->batch * cache->kv_heads;
+        err = launch_overlapping(kv_lengths_kernel, dim3((n + 255) / 256), 256, 0, s, a.length_out, cache->length, n);
+    }
+    return launched(err);
+}
+
+spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void* k, void* v, int tokens, long long batch_stride, long long token_stride,
+                         long long head_stride, void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace spqt;
+    spqt_status st = check_cache(cache);
+    if (st != SPQT_OK) return st;
+    if (!k || !v || tokens < 1 || batch_stride < 0 || token_stride < 0 || head_stride < 0) return SPQT_ERR_INVALID_ARG;
+    if (!aligned(k, 16) || !aligned(v, 16) || batch_stride % 8 || token_stride % 8 || head_stride % 8 || !aligned(length, 4)) return SPQT_ERR_ALIGNMENT;
+    if (cache->kv_heads * (cache->head_dim / 8) > 0x7fffffff / kReadTokens) return SPQT_ERR_UNSUPPORTED;
+    st = check_kv_workspace(workspace, workspace_bytes, kKvHeader);
+    if (st != SPQT_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int most = cache->table_width * cache->block_tokens;
+    if (tokens > most) tokens = most;
+    const ReadArgs a = {*cache, length ? length : cache->length, static_cast<__half*>(k), static_cast<__half*>(v), tokens, batch_stride, token_stride,
+                        head_stride, static_cast<int*>(status_word(workspace))};
+    const dim3 grid((unsigned)((tokens + kReadTokens - 1) / kReadTokens), (unsigned)cache->batch);
+#define SPQT_F(F, D) launch_overlapping(kv_read_kernel<F, D>, grid, 256, 0, s, a)
+    const cudaError_t err = SPQT_KV_DISPATCH(*cache, SPQT_F);
+#undef SPQT_F
+    return launched(err);
+}
+
+spqt_status spqt_kv_evict(const spqt_kv_cache* cache, int keep, int first, int recent, int32_t* table_out, int32_t* length_out, void* workspace,
+                          size_t workspace_bytes, void* stream)
+{
+    using namespace spqt;
+    spqt_status st = check_cache(cache);
+    if (st != SPQT_OK) return st;
+    if (!cache->weight || keep < 0 || first < 0 || recent < 0 || (long long)first + recent > keep) return SPQT_ERR_INVALID_ARG;
+    if (!aligned(table_out, 4) || !aligned(length_out, 4)) return SPQT_ERR_ALIGNMENT;
+    st = check_kv_workspace(workspace, workspace_bytes, kKvHeader);
+    if (st != SPQT_OK) return st;
+    const size_t smem = (size_t)cache->table_width * 8;
+    static thread_local int allowed_dev = -1;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return launched(cudaErrorInvalidDevice);
+    if (smem > 48 * 1024 && allowed_dev != dev) {
+        const cudaError_t err = cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxTableWidth * 8);
+        if (err != cudaSuccess) return launched(err);
+        allowed_dev = dev;
+    }
+    const EvictArgs a = {*cache, keep, first, recent, table_out, length_out, static_cast<int*>(status_word(workspace))};
+    return launched(launch_overlapping(kv_evict_kernel, dim3(cache->batch * cache->kv_heads), kEvictThreads, smem, static_cast<cudaStream_t>(stream), a));
+}
+
+spqt_status spqt_kv_status(const void* workspace, int* status_host, void* stream)
+{
+    if (!workspace || !status_host) return SPQT_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const void* const word = static_cast<const unsigned char*>(workspace) + spqt::kStatusOffset;
+    if (cudaMemcpyAsync(status_host, word, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
+        return spqt::launched(cudaErrorUnknown);
+    return *status_host == 0 ? SPQT_OK : SPQT_ERR_INVALID_ARG;
+}
+
+}  // extern "C"

@@ -10,8 +10,11 @@
 // 115 us).
 #include <Python.h>
 
+#include <cmath>
+
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -23,7 +26,7 @@ namespace {
 PyObject* g_error = nullptr;   // binding.SpqtError(status, where)
 
 struct Names {
-    PyObject *codes, *scale_zero, *records, *m, *n, *bits, *group, *cuda_stream;
+    PyObject *codes, *scale_zero, *records, *m, *n, *bits, *group, *cuda_stream, *desc, *device_index, *device;
 } g_names;
 
 // Leaves a call with a Python exception set.
@@ -407,6 +410,207 @@ PyObject* host_step_launch(PyObject*, Args a, Py_ssize_t na)
     });
 }
 
+// ---- the 8-bit cache and what is asked of logits
+
+// A KVCache object: the address of its spqt_kv_cache, the device of its buffers, which is the current one for the call.
+struct Cache {
+    const spqt_kv_cache* c;
+    int device;
+    c10::cuda::OptionalCUDAGuard guard;
+    explicit Cache(PyObject* p) : c(nullptr), device(int_attr(p, g_names.device_index))
+    {
+        PyObject* o = PyObject_GetAttr(p, g_names.desc);
+        if (!o) throw Raised();
+        c = static_cast<const spqt_kv_cache*>(PyLong_AsVoidPtr(o));
+        Py_DECREF(o);
+        if (!c) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "not a KVCache");
+            throw Raised();
+        }
+        guard.set_index((c10::DeviceIndex)device);
+    }
+    // a tensor of the cache's device
+    const at::Tensor& tensor(PyObject* o, at::ScalarType dtype, const char* name, bool contiguous = true) const
+    {
+        const at::Tensor& t = tensor_of(o, dtype, name, contiguous);
+        if (t.get_device() != device) raise(PyExc_ValueError, "%s must be on the cache's device", name);
+        return t;
+    }
+    void* optional(PyObject* o, at::IntArrayRef shape, const char* name) const
+    {
+        if (o == Py_None) return nullptr;
+        const at::Tensor& t = tensor(o, at::kInt, name);
+        if (t.sizes() != shape) raise(PyExc_ValueError, "%s has another shape than the cache's", name);
+        return t.data_ptr();
+    }
+    // [batch][tokens][heads][head_dim] whose heads lie side by side
+    const at::Tensor& rows(PyObject* o, int64_t heads, const char* name, bool packed_heads = true) const
+    {
+        const at::Tensor& t = tensor(o, at::kHalf, name, false);
+        if (t.dim() != 4 || t.size(0) != c->batch || t.size(1) < 1 || (heads > 0 && t.size(2) != heads) || t.size(3) != c->head_dim || t.stride(3) != 1 ||
+            (packed_heads && t.size(2) > 1 && t.stride(2) != c->head_dim)) {
+            PyErr_Format(PyExc_ValueError, packed_heads ? "%s must be [batch][tokens][heads][head_dim], the heads of a token side by side"
+                                                        : "%s must be [batch][tokens][kv_heads][head_dim] with unit stride in a row", name);
+            throw Raised();
+        }
+        return t;
+    }
+    void* stream(PyObject* o) const
+    {
+        if (o != Py_None) {
+            PyObject* d = PyObject_GetAttr(o, g_names.device_index);
+            if (d) {
+                Py_DECREF(d);
+                const int i = int_attr(o, g_names.device_index);
+                if (i != device) raise(PyExc_ValueError, "%s", "the stream is another device's");
+            } else {
+                PyErr_Clear();
+            }
+            return stream_of(o);
+        }
+        return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+    }
+};
+
+int64_t batch_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
+int64_t token_stride(const at::Tensor& t) { return t.size(1) > 1 ? t.stride(1) : 0; }
+
+int in_int(int64_t v, const char* name)
+{
+    if (v > 0x7fffffffLL) raise(PyExc_ValueError, "%s is too large", name);
+    return (int)v;
+}
+
+// (cache, k, v, workspace, counts, length_out, stream) -> the lengths
+PyObject* kv_append(PyObject*, Args a, Py_ssize_t na)
+{
+    return guarded([&]() -> PyObject* {
+        need_args(na, 7);
+        const Cache p(a[0]);
+        const at::Tensor &k = p.rows(a[1], p.c->kv_heads, "k"), &v = p.rows(a[2], p.c->kv_heads, "v");
+        if (k.size(1) != v.size(1) || batch_stride(k) != batch_stride(v) || token_stride(k) != token_stride(v))
+            raise(PyExc_ValueError, "%s", "k and v must have the same shape and strides");
+        const at::Tensor& ws = p.tensor(a[3], at::kByte, "workspace");
+        const void* counts = p.optional(a[4], {p.c->batch}, "counts");
+        void* out = p.optional(a[5], {p.c->batch, p.c->kv_heads}, "length_out");
+        void* s = p.stream(a[6]);
+        call("spqt_kv_append", [&] {
+            return spqt_kv_append(p.c, k.data_ptr(), v.data_ptr(), in_int(k.size(1), "the number of tokens"), batch_stride(k), token_stride(k),
+                                  static_cast<const int32_t*>(counts), static_cast<int32_t*>(out), ws.data_ptr(), (size_t)ws.numel(), s);
+        });
+        Py_RETURN_NONE;
+    });
+}
+
+// (cache, k, v, workspace, length, stream)
+PyObject* kv_read(PyObject*, Args a, Py_ssize_t na)
+{
+    return guarded([&]() -> PyObject* {
+        need_args(na, 6);
+        const Cache p(a[0]);
+        const at::Tensor &k = p.rows(a[1], p.c->kv_heads, "k", false), &v = p.rows(a[2], p.c->kv_heads, "v", false);
+        if (k.size(1) != v.size(1) || k.strides() != v.strides()) raise(PyExc_ValueError, "%s", "k and v must have the same shape and strides");
+        const at::Tensor& ws = p.tensor(a[3], at::kByte, "workspace");
+        const void* length = p.optional(a[4], {p.c->batch, p.c->kv_heads}, "length");
+        void* s = p.stream(a[5]);
+        call("spqt_kv_read", [&] {
+            return spqt_kv_read(p.c, static_cast<const int32_t*>(length), k.data_ptr(), v.data_ptr(), in_int(k.size(1), "the number of tokens"),
+                                batch_stride(k), token_stride(k), k.size(2) > 1 ? k.stride(2) : 0, ws.data_ptr(), (size_t)ws.numel(), s);
+        });
+        Py_RETURN_NONE;
+    });
+}
+
+// (cache, q, workspace, scale or None, accumulate, out, stream) -> out
+PyObject* kv_attention(PyObject*, Args a, Py_ssize_t na)
+{
+    return guarded([&]() -> PyObject* {
+        need_args(na, 7);
+        const Cache p(a[0]);
+        const at::Tensor& q = p.rows(a[1], 0, "q");
+        const at::Tensor& ws = p.tensor(a[2], at::kByte, "workspace");
+        const float scale = a[3] == Py_None ? (float)(1.0 / std::sqrt((double)p.c->head_dim)) : float_of(a[3]);
+        const int accumulate = PyObject_IsTrue(a[4]);
+        if (accumulate < 0) throw Raised();
+        at::Tensor out;
+        if (a[5] == Py_None) {
+            out = empty(q.sizes(), at::kHalf, q);
+        } else {
+            out = p.rows(a[5], q.size(2), "out");
+            if (out.size(1) != q.size(1)) raise(PyExc_ValueError, "%s", "out must have the shape of q");
+        }
+        void* s = p.stream(a[6]);
+        call("spqt_kv_attention", [&] {
+            return spqt_kv_attention(p.c, q.data_ptr(), batch_stride(q), token_stride(q), in_int(q.size(2), "the number of heads"),
+                                     in_int(q.size(1), "the number of queries"), scale, accumulate, out.data_ptr(), batch_stride(out), token_stride(out),
+                                     ws.data_ptr(), (size_t)ws.numel(), s);
+        });
+        return hand_back(a[5], out);
+    });
+}
+
+// (cache, keep, first, recent, workspace, table_out, length_out, stream)
+PyObject* kv_evict(PyObject*, Args a, Py_ssize_t na)
+{
+    return guarded([&]() -> PyObject* {
+        need_args(na, 8);
+        const Cache p(a[0]);
+        const int keep = int_of(a[1]), first = int_of(a[2]), recent = int_of(a[3]);
+        const at::Tensor& ws = p.tensor(a[4], at::kByte, "workspace");
+        void* table = p.optional(a[5], {p.c->batch, p.c->kv_heads, p.c->table_width}, "table_out");
+        void* length = p.optional(a[6], {p.c->batch, p.c->kv_heads}, "length_out");
+        void* s = p.stream(a[7]);
+        call("spqt_kv_evict", [&] {
+            return spqt_kv_evict(p.c, keep, first, recent, static_cast<int32_t*>(table), static_cast<int32_t*>(length), ws.data_ptr(), (size_t)ws.numel(), s);
+        });
+        Py_RETURN_NONE;
+    });
+}
+
+// (logits, tokens or None, top, entropy, stream) -> (logprob or None, entropy or None, top_logprob, top_index)
+PyObject* token_logprobs(PyObject*, Args a, Py_ssize_t na)
+{
+    return guarded([&]() -> PyObject* {
+        need_args(na, 5);
+        if (!THPVariable_Check(a[0])) raise(PyExc_TypeError, "%s must be a CUDA tensor", "logits");
+        const at::Tensor& x = THPVariable_Unpack(a[0]);
+        if (!x.is_cuda()) raise(PyExc_TypeError, "%s must be a CUDA tensor", "logits");
+        const at::ScalarType t = x.scalar_type();
+        if (t != at::kHalf && t != at::kBFloat16 && t != at::kFloat) raise(PyExc_TypeError, "%s must be float16, bfloat16 or float32", "logits");
+        if (x.dim() != 2 || (x.size(1) > 1 && x.stride(1) != 1)) raise(PyExc_ValueError, "%s", "logits must be [rows][vocab] with unit column stride");
+        const c10::cuda::OptionalCUDAGuard guard(x.device());
+        const int64_t rows = x.size(0);
+        const int top = int_of(a[2]);
+        if (top < 0) raise(PyExc_ValueError, "%s", "top must not be negative");
+        const int wants_entropy = PyObject_IsTrue(a[3]);
+        if (wants_entropy < 0) throw Raised();
+        const int32_t* tokens = nullptr;
+        const bool wants_logprob = a[1] != Py_None;
+        at::Tensor logprob, entropy;
+        if (wants_logprob) {
+            const at::Tensor& k = tensor_of(a[1], at::kInt, "tokens");
+            if (k.dim() != 1 || k.size(0) != rows || k.get_device() != x.get_device()) raise(PyExc_ValueError, "%s", "tokens must be [rows] on the device of logits");
+            tokens = static_cast<const int32_t*>(k.data_ptr());
+            logprob = empty({rows}, at::kFloat, x);
+        }
+        if (wants_entropy) entropy = empty({rows}, at::kFloat, x);
+        at::Tensor best = empty({rows, top}, at::kFloat, x), index = empty({rows, top}, at::kInt, x);
+        void* s = a[4] == Py_None ? c10::cuda::getCurrentCUDAStream(x.get_device()).stream() : stream_of(a[4]);
+        call("spqt_token_logprobs", [&] {
+            return spqt_token_logprobs(x.data_ptr(), t == at::kHalf ? SPQT_LOGITS_FP16 : t == at::kBFloat16 ? SPQT_LOGITS_BF16 : SPQT_LOGITS_FP32,
+                                       in_int(rows, "the number of rows"), in_int(x.size(1), "the vocabulary"), rows > 1 ? x.stride(0) : x.size(1), tokens, top,
+                                       wants_logprob ? static_cast<float*>(logprob.data_ptr()) : nullptr, wants_entropy ? static_cast<float*>(entropy.data_ptr()) : nullptr,
+                                       top > 0 ? static_cast<float*>(best.data_ptr()) : nullptr, top > 0 ? static_cast<int32_t*>(index.data_ptr()) : nullptr, s);
+        });
+        auto wrapped = [](bool there, at::Tensor& v) {
+            if (there) return THPVariable_Wrap(std::move(v));
+            Py_INCREF(Py_None);
+            return Py_None;
+        };
+        return tuple_of(wrapped(wants_logprob, logprob), wrapped(wants_entropy, entropy), THPVariable_Wrap(std::move(best)), THPVariable_Wrap(std::move(index)));
+    });
+}
+
 PyObject* set_error(PyObject*, PyObject* cls)
 {
     Py_INCREF(cls);
@@ -418,7 +622,8 @@ PyObject* set_error(PyObject*, PyObject* cls)
 PyMethodDef g_methods[] = {
     SPQT_METHOD(sparsify), SPQT_METHOD(sparse_gemv), SPQT_METHOD(sparsify_gemv), SPQT_METHOD(dense_gemv),
     SPQT_METHOD(sparse_gemm_small), SPQT_METHOD(dense_gemm_small), SPQT_METHOD(kqw_sparse_gemv), SPQT_METHOD(kqw_dense_gemv), SPQT_METHOD(pack),
-    SPQT_METHOD(kqw_pack), SPQT_METHOD(host_step_launch),
+    SPQT_METHOD(kqw_pack), SPQT_METHOD(host_step_launch), SPQT_METHOD(kv_append), SPQT_METHOD(kv_read), SPQT_METHOD(kv_attention),
+    SPQT_METHOD(kv_evict), SPQT_METHOD(token_logprobs),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -430,6 +635,7 @@ PyMODINIT_FUNC PyInit__native(void)
 {
     g_names = {PyUnicode_InternFromString("codes"), PyUnicode_InternFromString("scale_zero"), PyUnicode_InternFromString("records"),
                PyUnicode_InternFromString("m"), PyUnicode_InternFromString("n"), PyUnicode_InternFromString("bits"),
-               PyUnicode_InternFromString("group"), PyUnicode_InternFromString("cuda_stream")};
+               PyUnicode_InternFromString("group"), PyUnicode_InternFromString("cuda_stream"), PyUnicode_InternFromString("desc"),
+               PyUnicode_InternFromString("device_index"), PyUnicode_InternFromString("device")};
     return PyModule_Create(&g_module);
 }
