@@ -10,10 +10,11 @@
 // registers (a byte permutation and a subtraction, or one conversion from e4m3).  Scales stay outside of the product: a block's k scale multiplies its scores,
 // its v scale the probabilities.
 //
-// Probabilities are needed in fp16: p = 2^(s + e - M + 14), s the score in powers of two, 2^e the power of two in the v scale, M the
-// largest s + e so far.  p then lies in 0 .. 2^14, and what 16 bits cannot hold of it (2^-11) enters as a second fp16 value: with up
-// to four rows in the columns that they leave free, else in a second instruction.  Without it the result is 1.4 times as far from
-// the exact one, as far as its own rounding to fp16 takes it.  Sums are fp32 and know nothing of v's scales.
+// Probabilities are needed in fp16: p = 2^(s + e - M + 10), s the score in powers of two, 2^e the power of two in the v scale, M the
+// largest s + e when it was last looked at, which is when one exceeds it by 4: lanes need not ask one another for the largest of a
+// tile.  p then lies in 0 .. 2^14, and what 16 bits cannot hold of it (2^-11) enters as a second fp16 value: with up to four rows in
+// the columns that they leave free, else in a second instruction.  Without it the result is 1.4 times as far from the exact one,
+// as far as its own rounding to fp16 takes it.  Sums are fp32 and know nothing of v's scales.
 //
 // Work: the tiles (32 tokens) of all streams are laid end to end and cut into equal parts, one per CTA; the warps of a CTA take its
 // tiles in turn, each with a ring of tiles on their way (cp.async, so that a block number is all that is needed ahead).  A stream
@@ -31,7 +32,8 @@ namespace spqt {
 constexpr int kTile = 32;               // tokens of a tile of codes; half as many of the block that is not full
 constexpr int kMaxAttnCtas = 320;       // parts at most
 constexpr int kLengthCache = 1024;      // streams whose lengths a CTA keeps in shared memory
-constexpr float kUp = 14.0f;            // p of the largest score is 2^kUp
+constexpr float kUp = 10.0f;            // p of the largest score is 2^kUp, when M is set
+constexpr float kSlack = 4.0f;          // and 2^(kUp + kSlack) before M is set anew
 
 struct AttnArgs {
     spqt_kv_cache c;
@@ -41,6 +43,7 @@ struct AttnArgs {
     long long out_batch, out_token;
     int group, queries, rows;           // rows = group * queries of a stream, row i * group + g
     int row_groups;                     // of ROWS rows
+    int shift;                          // log2 of the tokens of a block
     int accumulate;
     float scale_log2;
     int* status;
@@ -54,20 +57,21 @@ template <int D, int ROWS>
 struct AttnShape {
     static constexpr int kWarps = D == 256 ? 4 : 8;
     static constexpr int kTileBytes = 2 * kTile * D;
-    static constexpr int kStages = D == 64 ? 4 : (D >= 128 && ROWS == 16) ? 2 : 3;
+    static constexpr int kStages = D <= 96 ? 4 : D == 128 ? 2 : ROWS == 16 ? 2 : 3;
     static constexpr int kCols = ROWS == 16 ? 2 : 1;             // sets of eight columns
     static constexpr int kStride = D + 4;                        // of a row of sums in shared memory: 8 bytes a lane without conflicts
 };
 
-// Tiles of a stream of n tokens: full blocks by 32 tokens, then the open one by 16.
-__device__ __forceinline__ int code_tiles(int n, int bt) { return (n / bt * bt + kTile - 1) / kTile; }
-__device__ __forceinline__ int tiles_of(int n, int bt) { return code_tiles(n, bt) + (n % bt + 15) / 16; }
+// Tokens of a stream's full blocks, and its tiles: those by 32 tokens, then the open block's by 16.
+__device__ __forceinline__ int full_tokens(int n, int shift) { return n >> shift << shift; }
+__device__ __forceinline__ int code_tiles(int n, int shift) { return (full_tokens(n, shift) + kTile - 1) / kTile; }
+__device__ __forceinline__ int tiles_of(int n, int shift) { return code_tiles(n, shift) + (n - full_tokens(n, shift) + 15) / 16; }
 
-// CTAs that work: not more than leave a tile for every warp.  A CTA's tiles begin at total * i / ctas.
-__device__ __forceinline__ int working_ctas(long long total, int warps, int most)
+// CTAs that work: not more than leave a tile for every warp, unless there are more segments.  A CTA's tiles begin at
+// total * i / ctas.
+__device__ __forceinline__ int working_ctas(int total, int segments, int warps, int most)
 {
-    const long long c = (total + warps - 1) / warps;
-    return (int)(c < most ? (c < 1 ? 1 : c) : most);
+    return min(max(max((total + warps - 1) / warps, min(segments, total)), 1), most);
 }
 __device__ __forceinline__ int owner_of(long long tile, long long total, int ctas) { return (int)(((tile + 1) * ctas - 1) / total); }
 
@@ -110,14 +114,25 @@ __device__ __forceinline__ unsigned halves(float a, float b)
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const unsigned*>(&h);
 }
-// 16 bytes, or zeros
-__device__ __forceinline__ void cp_async_16_if(bool on, unsigned dst, const void* src)
+// 16 bytes, or zeros where `bytes` is 0
+__device__ __forceinline__ void cp_async_16_of(unsigned dst, const void* src, int bytes)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void cp_async_scale(unsigned dst, const void* src)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// Where a 16-byte piece of a row of N lies in a tile: as in memory, so that the pieces of neighbouring lanes of a copy lie within the
+// same 128 bytes (a copy whose lanes write 32 places takes 32 turns: the whole call 100 instead of 56 us with 131072 tokens), but
+// exchanged among them by the row, so that the same piece of eight rows, which ldmatrix reads at once, lies in eight places.
+template <int N>
+__device__ __forceinline__ unsigned place_of(int row, int piece)
+{
+    const int turn = N % 8 == 0 ? row & 7 : N % 4 == 0 ? row >> 1 & 3 : row >> 2 & 1;
+    if (N % 8 == 0) return (unsigned)(row * N * 16 + (((piece & 7) ^ turn) + (piece & ~7)) * 16);
+    return (unsigned)((row * N + piece) ^ turn) * 16;
 }
 
 template <int FMT, int D, int ROWS>
@@ -133,7 +148,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
     __shared__ __align__(16) float s_o[NW / 2][ROWS][S::kStride];
     const spqt_kv_cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, cc = lane & 3;
-    const int bt = c.block_tokens;
+    const int shift = a.shift;
     const unsigned ring = smem_u32(s_ring) + warp * STAGES * S::kTileBytes;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -146,7 +161,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         if (st < streams) {
             const int n = length_or_none((int)ld_global_u32(c.length + st), c, a.status);
             if (st < kLengthCache) s_len[st] = n;
-            mine += tiles_of(n, bt) * a.row_groups;
+            mine += tiles_of(n, shift) * a.row_groups;
         }
     }
     int incl = mine;
@@ -164,11 +179,11 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         total += s_scan[w];
     }
     auto length_of = [&](int st) { return st < kLengthCache ? s_len[st] : length_or_none((int)ld_global_u32(c.length + st), c, a.status); };
-    const int ctas = working_ctas(total, NW, gridDim.x), cta = blockIdx.x;
+    const int ctas = working_ctas(total, streams * a.row_groups, NW, gridDim.x), cta = blockIdx.x;
     if (cta == 0) {                           // for the second kernel
         if (tid == 0) a.begin[streams * a.row_groups] = total;
         for (int st = tid * per, at = base; st < min(streams, (tid + 1) * per); ++st) {
-            const int k = tiles_of(length_of(st), bt);
+            const int k = tiles_of(length_of(st), shift);
             for (int r = 0; r < a.row_groups; ++r, at += k) a.begin[st * a.row_groups + r] = at;
         }
     }
@@ -177,7 +192,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
     if (t0 >= base && t0 < base + mine) {
         int st = tid * per, at = base;
         for (;; ++st) {
-            const int k = tiles_of(length_of(st), bt) * a.row_groups;
+            const int k = tiles_of(length_of(st), shift) * a.row_groups;
             if (t0 < at + k) break;
             at += k;
         }
@@ -185,7 +200,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         s_start[1] = at;
     }
     __syncthreads();
-    const int stream0 = s_start[0], n0 = length_of(stream0), tiles0 = tiles_of(n0, bt), rg0 = (t0 - s_start[1]) / tiles0;
+    const int stream0 = s_start[0], n0 = length_of(stream0), tiles0 = tiles_of(n0, shift), rg0 = (t0 - s_start[1]) / tiles0;
     const int seg0 = stream0 * a.row_groups + rg0, begin0 = s_start[1] + rg0 * tiles0;
 
     // ---- the tiles ahead: a walk over this warp's tiles that knows the segment of each; first the block numbers, one tile later
@@ -196,11 +211,12 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             ++w_seg;
             w_begin = w_end;
             w_n = length_of(w_seg / a.row_groups);
-            w_end = w_begin + tiles_of(w_n, bt);
+            w_end = w_begin + tiles_of(w_n, shift);
         }
     };
     seek();
-    int p_tile = w_tile, p_stream = 0, p_local = 0, p_n = 0, p_id = 0;     // the tile whose block numbers are on their way (lane u: half u)
+    // the tile whose block numbers are on their way (lane u: half u)
+    int p_tile = w_tile, p_stream = 0, p_local = 0, p_n = 0, p_id = 0;
     auto look_up = [&]() {
         p_tile = w_tile;
         if (w_tile < t1) {
@@ -208,52 +224,56 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             p_local = w_tile - w_begin;
             p_n = w_n;
             const int token = p_local * kTile + (lane & 1) * 16;
-            p_id = token < w_n / bt * bt ? (int)ld_global_u32(c.table + (size_t)p_stream * c.table_width + token / bt) : 0;
+            p_id = token < full_tokens(w_n, shift) ? (int)ld_global_u32(c.table + (size_t)p_stream * c.table_width + (token >> shift)) : 0;
             w_tile += NW;
-            seek();
+            if (w_tile >= w_end) seek();
         }
     };
+    // A lane's pieces of a half tile of codes; those of eight rows and more apart lie as far apart.
+    constexpr int kDistinct = CH == 4 ? 1 : CH == 8 ? 2 : CH == 16 ? 4 : D / 32;
+    unsigned place[kDistinct];
+#pragma unroll
+    for (int i = 0; i < kDistinct; ++i) place[i] = place_of<CH>((i * 32 + lane) / CH, (i * 32 + lane) % CH);
     auto copy = [&](int stage) {
         if (p_tile >= t1) return;
         const unsigned dst = ring + stage * S::kTileBytes;
-        const int full = p_n / bt * bt, nt = (full + kTile - 1) / kTile;
-        if (p_local < nt) {
+        const int full = full_tokens(p_n, shift), tail = p_local - (full + kTile - 1) / kTile;
+        if (tail < 0) {
             const bool known = (unsigned)p_id < (unsigned)c.blocks;
             const int id = known ? p_id : 0;
             if (!known) refuse(a.status);
-            const unsigned at = smem_u32(&s_scale[warp][stage][0]);
             if (lane < 4) {
                 // (lanes 0 and 1: k of the halves, 2 and 3: v of the halves; lane & 1 is the half whose number the lane holds)
-                if (known) cp_async_scale(at + lane * 4, (lane < 2 ? c.k_scale : c.v_scale) + id);
-                else sts_u32(at + lane * 4, 0x7fffffffu);
+                const unsigned at = smem_u32(&s_scale[warp][stage][0]) + lane * 4;
+                if (known) cp_async_scale(at, (lane < 2 ? c.k_scale : c.v_scale) + id);
+                else sts_u32(at, 0x7fffffffu);
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int token = p_local * kTile + u * 16;
-                const bool on = token < full;
-                const size_t from = ((size_t)__shfl_sync(0xffffffffu, id, u) * bt + token % bt) * D;
-                const unsigned char* const k = static_cast<const unsigned char*>(c.k_codes) + from + lane * 16;
-                const unsigned char* const v = static_cast<const unsigned char*>(c.v_codes) + from + lane * 16;
+                const int bytes = u == 0 || token < full ? 16 : 0;
+                const size_t from = (((size_t)(unsigned)__shfl_sync(0xffffffffu, id, u) << shift) + (token & ((1 << shift) - 1))) * D + lane * 16;
+                const unsigned char* const k = static_cast<const unsigned char*>(c.k_codes) + from;
+                const unsigned char* const v = static_cast<const unsigned char*>(c.v_codes) + from;
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
-                    const int p = i * 32 + lane, r = p / CH, ch = p % CH;
-                    const unsigned to = dst + (unsigned)(ch * kTile + ((u * 16 + r) ^ (ch & 7))) * 16;
-                    cp_async_16_if(on, to, k + i * 512);
-                    cp_async_16_if(on, to + kTile * D, v + i * 512);
+                    const unsigned to = dst + place[i % kDistinct] + (unsigned)(i / kDistinct * kDistinct * 512 + u * 16 * D);
+                    cp_async_16_of(to, k + i * 512, bytes);
+                    cp_async_16_of(to + kTile * D, v + i * 512, bytes);
                 }
             }
         } else {
-            const int r0 = (p_local - nt) * 16;
-            const size_t from = ((size_t)p_stream * bt + r0) * D;
+            const int r0 = tail * 16;
+            const size_t from = (((size_t)p_stream << shift) + r0) * D;
             const __half* const k = static_cast<const __half*>(c.k_tail) + from + lane * 8;
             const __half* const v = static_cast<const __half*>(c.v_tail) + from + lane * 8;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
                 const int p = i * 32 + lane, r = p / (D / 8), ch = p % (D / 8);
-                const unsigned to = dst + (unsigned)(ch * 16 + (r ^ (ch & 7))) * 16;
-                const bool on = full + r0 + r < p_n;
-                cp_async_16_if(on, to, k + i * 256);
-                cp_async_16_if(on, to + kTile * D, v + i * 256);
+                const unsigned to = dst + place_of<2 * CH>(r, ch);
+                const int bytes = full + r0 + r < p_n ? 16 : 0;
+                cp_async_16_of(to, k + i * 256, bytes);
+                cp_async_16_of(to + kTile * D, v + i * 256, bytes);
             }
         }
     };
@@ -269,7 +289,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
     int stage = 0, tile = t0 + warp;
     int seg = seg0, begin = begin0, n = n0;
     while (begin < t1) {
-        const int tiles = tiles_of(n, bt), end = begin + tiles;
+        const int tiles = tiles_of(n, shift), end = begin + tiles;
         if (tiles == 0) {
             ++seg;
             n = length_of(seg / a.row_groups);
@@ -299,13 +319,14 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                 lim[s][e] = rc < a.rows ? n - a.queries + 1 + rc / a.group : n;
             }
         }
-        const int least = n - a.queries + 1;  // what all rows see
-        const int full = n / bt * bt, nt = (full + kTile - 1) / kTile;
+        const int full = full_tokens(n, shift), nt = (full + kTile - 1) / kTile;
+        const int clean = max(0, min(full, n - a.queries + 1)) / kTile;   // tiles of whose tokens all are there and all rows see all
         float o[CH][NC][4];
-        float M[NC][2], l[NC][2];
+        float M[NC][2], less[NC][2], l[NC][2];   // less: M - kUp, finite
 #pragma unroll
         for (int s = 0; s < NC; ++s) {
             M[s][0] = M[s][1] = -INFINITY;
+            less[s][0] = less[s][1] = 0.0f;
             l[s][0] = l[s][1] = 0.0f;
 #pragma unroll
             for (int d = 0; d < CH; ++d) o[d][s][0] = o[d][s][1] = o[d][s][2] = o[d][s][3] = 0.0f;
@@ -337,7 +358,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
 #pragma unroll
                 for (int j = 0; j < CH; ++j) {
                     unsigned r[4], f[4][2];
-                    ldsm_x4(at + (unsigned)(j * kTile + (lane ^ (j & 7))) * 16, r);
+                    ldsm_x4(at + place_of<CH>(lane, j), r);
 #pragma unroll
                     for (int m = 0; m < 4; ++m) widen<FMT, false>(r[m], f[m][0], f[m][1]);
 #pragma unroll
@@ -350,42 +371,15 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
 #pragma unroll
                 for (int j = 0; j < CH; ++j) {
                     const int ch = 2 * j + (cc >> 1);
-                    const uint2 r0 = lds_v2(at + (unsigned)(ch * 16 + (g ^ (ch & 7))) * 16 + (cc & 1) * 8);
-                    const uint2 r1 = lds_v2(at + (unsigned)(ch * 16 + ((g + 8) ^ (ch & 7))) * 16 + (cc & 1) * 8);
+                    const uint2 r0 = lds_v2(at + place_of<2 * CH>(g, ch) + (cc & 1) * 8);
+                    const uint2 r1 = lds_v2(at + place_of<2 * CH>(g + 8, ch) + (cc & 1) * 8);
 #pragma unroll
                     for (int s = 0; s < NC; ++s) mma_16816(x[s][0], r0.x, r1.x, r0.y, r1.y, qf[s][j][0], qf[s][j][1]);
                 }
             }
-            // scores in powers of two; the v scale as 2^ve * vf, a scale of zero (or below the normal numbers) with ve = 0
+            // scores in powers of two, with the v scale as 2^ve * vf (one that is zero, below the normal numbers or not finite: ve = 0)
             float ve[2], vf[2], down[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const unsigned bits = __float_as_uint(vs[u]), ex = bits >> 23 & 0xffu;
-                const bool plain = ex != 0u && ex != 0xffu;
-                ve[u] = plain ? (float)((int)ex - 127) : 0.0f;
-                vf[u] = plain ? __uint_as_float((bits & 0x807fffffu) | 0x3f800000u) : vs[u];
-                down[u] = plain ? __uint_as_float((254u - ex) << 23) : 1.0f;      // 2^-ve
-                const float f = ks[u] * a.scale_log2;
-#pragma unroll
-                for (int s = 0; s < NC; ++s)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[s][u][e] *= f;
-            }
-            const int tokens = codes ? kTile : 16;
-            if (token0 + tokens > least || (codes && token0 + kTile > full) || !codes) {
-                // (a half tile behind the last full block counts for the next kind of tile)
-                const int seen = codes ? full : n;
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int token = token0 + u * 16 + (e >> 1) * 8 + g;
-                        const bool in = token < seen && (codes || u == 0);
-#pragma unroll
-                        for (int s = 0; s < NC; ++s)
-                            if (!in || token >= lim[s][e & 1]) x[s][u][e] = -INFINITY;
-                    }
-            }
+            bool plain = true;
             if (a.accumulate) {
                 float* const to = a.scores + (size_t)tile * (kTile * ROWS);
                 if (ROWS >= 8 || cc < 2) {
@@ -393,29 +387,69 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                     for (int s = 0; s < NC; ++s)
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            *reinterpret_cast<float2*>(to + (u * 16 + g) * ROWS + s * 8 + 2 * cc) = make_float2(x[s][u][0], x[s][u][1]);
-                            *reinterpret_cast<float2*>(to + (u * 16 + g + 8) * ROWS + s * 8 + 2 * cc) = make_float2(x[s][u][2], x[s][u][3]);
+                            const float f = ks[u] * a.scale_log2;
+                            float v[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] = token0 + u * 16 + (e >> 1) * 8 + g < lim[s][e & 1] ? x[s][u][e] * f : -INFINITY;
+                            *reinterpret_cast<float2*>(to + (u * 16 + g) * ROWS + s * 8 + 2 * cc) = make_float2(v[0], v[1]);
+                            *reinterpret_cast<float2*>(to + (u * 16 + g + 8) * ROWS + s * 8 + 2 * cc) = make_float2(v[2], v[3]);
                         }
                 }
             }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const unsigned bits = __float_as_uint(vs[u]), ex = bits >> 23 & 0xffu;
+                const bool p = ex != 0u && ex != 0xffu;
+                plain = plain && p;
+                ve[u] = p ? (float)((int)ex - 127) : 0.0f;
+                vf[u] = p ? __uint_as_float((bits & 0x807fffffu) | 0x3f800000u) : vs[u];
+                down[u] = p ? __uint_as_float((254u - ex) << 23) : 1.0f;      // 2^-ve
+                const float f = ks[u] * a.scale_log2;
+#pragma unroll
+                for (int s = 0; s < NC; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[s][u][e] = fmaf(x[s][u][e], f, ve[u]);
+            }
+            if (local >= clean) {
+                // (a half tile behind the last full block counts for the next kind of tile)
+                const int there = codes ? full : n;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int token = token0 + u * 16 + (e >> 1) * 8 + g;
+                        const bool in = token < there && (codes || u == 0);
+#pragma unroll
+                        for (int s = 0; s < NC; ++s)
+                            if (!in || token >= lim[s][e & 1]) x[s][u][e] = -INFINITY;
+                    }
+            }
             unsigned ph[NC][2][2], pl[NC][2][2];
-            float alpha[NC][2];
-            bool rescale = false;
+            float top[NC][2];
+            bool above = false;
 #pragma unroll
             for (int s = 0; s < NC; ++s)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float m = fmaxf(fmaxf(x[s][0][e], x[s][0][e + 2]) + ve[0], fmaxf(x[s][1][e], x[s][1][e + 2]) + ve[1]);
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                    m = fmaxf(m, M[s][e]);
-                    alpha[s][e] = m == M[s][e] ? 1.0f : exp2_fast(M[s][e] - m);
-                    rescale = rescale || m != M[s][e];
-                    M[s][e] = m;
-                    l[s][e] *= alpha[s][e];
+                    top[s][e] = fmaxf(fmaxf(x[s][0][e], x[s][0][e + 2]), fmaxf(x[s][1][e], x[s][1][e + 2]));
+                    above = above || top[s][e] > M[s][e] + kSlack;
                 }
-            if (__any_sync(0xffffffffu, rescale)) {
+            if (__any_sync(0xffffffffu, above)) {
+                float alpha[NC][2];
+#pragma unroll
+                for (int s = 0; s < NC; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float m = top[s][e];
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                        m = fmaxf(m, M[s][e]);
+                        alpha[s][e] = m == M[s][e] ? 1.0f : exp2_fast(M[s][e] - m);
+                        M[s][e] = m;
+                        less[s][e] = m == -INFINITY ? 0.0f : m - kUp;
+                        l[s][e] *= alpha[s][e];
+                    }
 #pragma unroll
                 for (int d = 0; d < CH; ++d)
 #pragma unroll
@@ -430,10 +464,13 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                     float w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float m = M[s][e & 1];
-                        const float p = exp2_fast(x[s][u][e] + (ve[u] + kUp - (m == -INFINITY ? 0.0f : m)));
+                        const float p = exp2_fast(x[s][u][e] - less[s][e & 1]);
                         l[s][e & 1] = fmaf(p, down[u], l[s][e & 1]);
-                        w[e] = x[s][u][e] == -INFINITY ? 0.0f : p * vf[u];   // (whatever the v scale of what is not seen)
+                        w[e] = p * vf[u];
+                    }
+                    if (!plain) {             // (what is not seen is nothing, whatever its block's scale)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = x[s][u][e] == -INFINITY ? 0.0f : w[e];
                     }
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
@@ -452,7 +489,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
 #pragma unroll
                 for (int d = 0; d < CH; ++d) {
                     unsigned r[4], f[4][2];
-                    ldsm_x4_trans(at + kTile * D + (unsigned)(d * kTile + (lane ^ (d & 7))) * 16, r);
+                    ldsm_x4_trans(at + kTile * D + place_of<CH>(lane, d), r);
 #pragma unroll
                     for (int m = 0; m < 4; ++m) widen<FMT, true>(r[m], f[m][0], f[m][1]);
 #pragma unroll
@@ -470,7 +507,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                     const int ch = 2 * d + (g >> 2);
                     unsigned w[4];
                     bool odd = false;             // values that are not finite: out of the product, and to the rows that see them
-                    auto word = [&](int token) { return lds_u32(at + kTile * D + (unsigned)(ch * 16 + (token ^ (ch & 7))) * 16 + (g & 3) * 4); };
+                    auto word = [&](int token) { return lds_u32(at + kTile * D + place_of<2 * CH>(token, ch) + (g & 3) * 4); };
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         w[k] = word(2 * cc + (k & 1) + (k >> 1) * 8);
@@ -633,16 +670,16 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(cons
     __shared__ float s_o[kJoinWarps][D];
     __shared__ float2 s_ml[64];
     const spqt_kv_cache& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bt = c.block_tokens;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, shift = a.shift;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int segments = streams * a.row_groups, total = (int)ld_global_u32(a.begin + segments);
-    const int ctas = working_ctas(total, warps, parts);
+    const int ctas = working_ctas(total, segments, warps, parts);
     if ((int)blockIdx.x < rows_ctas) {
         const int rr = blockIdx.x % a.rows, stream = blockIdx.x / a.rows, rg = rr / ROWS, r = rr % ROWS, seg = stream * a.row_groups + rg;
         const int b = stream / c.kv_heads, h = stream % c.kv_heads, qi = rr / a.group;
         const int begin = (int)ld_global_u32(a.begin + seg);   // (of an empty stream: of no meaning)
-        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, bt);
+        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, shift);
         __half* const out = a.out + (long long)b * a.out_batch + (long long)qi * a.out_token + ((long long)h * a.group + (rr - qi * a.group)) * D;
         if (tiles == 0) {
             for (int d = tid * 2; d < D; d += kJoinWarps * 64) *reinterpret_cast<unsigned*>(out + d) = 0u;
@@ -697,13 +734,13 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(cons
         left = min(step, left - k);
     }
     for (int t = t0; t < t1;) {
-        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, bt);
+        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, shift);
         if (tiles == 0) {
             ++stream;
             continue;
         }
         const int seg = stream * a.row_groups, begin = (int)ld_global_u32(a.begin + seg), first = begin / a.row_groups;
-        const int stop = min(t1, first + tiles), full = n / bt * bt, nt = (full + kTile - 1) / kTile;
+        const int stop = min(t1, first + tiles), full = full_tokens(n, shift), nt = (full + kTile - 1) / kTile;
         const int32_t* const row = c.table + (size_t)stream * c.table_width;
         for (int rb = 0; rb < a.rows; rb += 64) {      // 64 rows at a time
             const int rows = min(64, a.rows - rb);
@@ -719,7 +756,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(cons
                 const bool codes = local < nt;
                 const int token = (codes ? local * kTile : full + (local - nt) * 16) + lane;
                 if (token >= (codes ? full : n) || (!codes && lane >= 16)) continue;
-                const unsigned block = (unsigned)row[token / bt];
+                const unsigned block = (unsigned)row[token >> shift];
                 if (block >= (unsigned)c.blocks) {
                     refuse(a.status);
                     continue;
@@ -733,7 +770,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(cons
                     for (int k = 0; k < 4; ++k)
                         if (r + k < rows) sum = fmaf(exp2_fast(e[k] - s_ml[r + k].x), s_ml[r + k].y, sum);
                 }
-                c.weight[(size_t)block * bt + token % bt] += sum;
+                c.weight[((size_t)block << shift) + (token & ((1 << shift) - 1))] += sum;
             }
         }
         t = stop;
@@ -856,7 +893,7 @@ spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long lo
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     const int group = q_heads / cache->kv_heads, rows = group * queries, R = rows_of(rows);
     const AttnArgs a = {*cache, static_cast<const __half*>(q), q_batch_stride, q_token_stride, static_cast<__half*>(out), out_batch_stride, out_token_stride,
-                        group, queries, rows, (rows + R - 1) / R, accumulate ? 1 : 0, scale * 1.4426950408889634f, static_cast<int*>(status_word(workspace)),
+                        group, queries, rows, (rows + R - 1) / R, 31 - __builtin_clz((unsigned)cache->block_tokens), accumulate ? 1 : 0, scale * 1.4426950408889634f, static_cast<int*>(status_word(workspace)),
                         reinterpret_cast<int*>(ws + w.begin), reinterpret_cast<float2*>(ws + w.ml), reinterpret_cast<float*>(ws + w.o),
                         reinterpret_cast<float*>(ws + w.scores)};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
