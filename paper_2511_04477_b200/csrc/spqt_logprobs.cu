@@ -1,15 +1,17 @@
 // What a row of logits says about a token: its log probability, the row's entropy, the largest log probabilities with their
 // places; one pass over the logits, nothing of the size of the row written.
 //
-// A CTA (or each of the CTAs of a cluster, for a part of a row) takes its values from global memory once, into shared memory as
-// they come; on the way a thread keeps its maximum m, the sum S of e^(x-m) and, for the entropy, the sum T of e^(x-m) (x-m).
-// H = log S - T / S.  (x - m is exact for the largest, so that a token without alternatives has log probability and entropy zero.)
-// Memory bounds many rows (one exponential and eight instructions a value are close behind), the chain of steps a few.
+// A row is read once, by a CTA, by the CTAs of a cluster (few rows: a part each) or by a warp (short rows).  On the way a thread keeps
+// its maximum m, the sum S of e^(x-m) and, for the entropy, the sum T of e^(x-m) (x-m).  H = log S - T / S.  (x - m is exact for the
+// largest, so that a token without alternatives has log probability and entropy zero.)  Memory bounds many rows, with the
+// instructions close behind (an exponential and five more a value, two values an instruction where there is one for two), the
+// chain of steps a few.
 //
-// The largest `top` of a part: of each warp the q-th largest of its threads' maxima, the least of these over the warps: q times the
-// warps threads reach it, so that at least `top` values do, and hardly more than a hundred.  They are listed, and each finds its
-// place by counting those before it.  Where more values reach the bound than the list holds (many equal ones), the top-th value
-// is searched bit by bit.  Equal values count in the order of their places throughout: a value and its place are one number.
+// The largest `top` of a part: every warp names the largest few of its threads' maxima, and the top-th largest of those named is a
+// bound that `top` values or more reach, hardly more in most rows.  Only the threads that reach it have their values looked at again;
+// these are listed, and each finds its place by counting those before it.  Where more reach the bound than the list holds
+// (many equal ones), the top-th value is searched bit by bit.  Equal values count in the order of their places throughout: a value
+// and its place are one number.
 #include <cuda_bf16.h>
 
 #include "spqt_common.cuh"
@@ -19,10 +21,10 @@
 namespace spqt {
 
 constexpr int kMaxTop = 32, kMaxVocab = 1 << 20;
-constexpr int kLogThreads = 512, kLogWarps = kLogThreads / 32;
 constexpr int kMaxLogCtas = 8;          // of a cluster
+constexpr int kNamed = 64;              // maxima that the warps name: 4 of each, or more of fewer warps
 constexpr int kLogList = 1536;          // values that may reach the bound
-constexpr size_t kLogKeep = 98304;      // bytes of a part that shared memory keeps; larger ones are read again
+constexpr int kWarpVocab = 4096;        // rows up to which a warp does one alone
 
 struct LogArgs {
     const void* logits;
@@ -30,7 +32,7 @@ struct LogArgs {
     const int32_t* tokens;
     float *logprob, *entropy, *top_logprob;
     int32_t* top_index;
-    int vocab, top, part, keep;         // part: values of a CTA; keep: they stay in shared memory
+    int vocab, top, part;               // part: values of a CTA of a cluster
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -50,12 +52,13 @@ __device__ __forceinline__ float value_of(unsigned k)
 __device__ __forceinline__ unsigned long long key_of(float f, int place) { return (unsigned long long)value_bits(f) << 32 | (unsigned)(0x7fffffff - place); }
 __device__ __forceinline__ int place_of(unsigned long long key) { return 0x7fffffff - (int)(unsigned)key; }
 
-__device__ __forceinline__ float exp_of(float x)
+__device__ __forceinline__ float exp2_of(float x)
 {
     float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float exp_of(float x) { return exp2_of(x * kLog2e); }
 
 struct Sums {
     float m, s, t;                      // m = -infinity: nothing summed
@@ -68,272 +71,448 @@ __device__ __forceinline__ void move_to(Sums& a, float m)   // to a maximum not 
     a.s *= f;
     a.m = m;
 }
-__device__ __forceinline__ Sums joined(Sums a, Sums b)
+// over the lanes of a warp (in all of them)
+__device__ __forceinline__ Sums joined(Sums a)
 {
-    const float m = fmaxf(a.m, b.m);
+    float m = a.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     move_to(a, m);
-    move_to(b, m);
-    return {m, a.s + b.s, a.t + b.t};
-}
-__device__ __forceinline__ Sums shuffled(const Sums& a, int o)
-{
-    return {__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o), __shfl_xor_sync(0xffffffffu, a.t, o)};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+        a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
+    }
+    return a;
 }
 
+// 16 bytes of values: two fp32 values in a register pair each, and their largest (not-a-number left out).
 template <class T>
-struct Vec {                            // 16 bytes of values
-    static constexpr int N = 16 / (int)sizeof(T);
-    float x[N];
+struct Vec {
+    static constexpr int N = 16 / (int)sizeof(T), P = N / 2;
+    unsigned long long x[P];
+    float top;
     __device__ __forceinline__ explicit Vec(const uint4& w)
     {
         const unsigned u[4] = {w.x, w.y, w.z, w.w};
+        if constexpr (sizeof(T) == 4) {
+            x[0] = pack2(__uint_as_float(u[0]), __uint_as_float(u[1]));
+            x[1] = pack2(__uint_as_float(u[2]), __uint_as_float(u[3]));
+            top = fmaxf(fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])), fmaxf(__uint_as_float(u[2]), __uint_as_float(u[3])));
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const __half2* h = reinterpret_cast<const __half2*>(u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) {
-                x[i] = __uint_as_float(u[i]);
-            } else if constexpr (std::is_same<T, __half>::value) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
-                x[2 * i] = f.x, x[2 * i + 1] = f.y;
-            } else {
-                x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = __half22float2(h[i]);
+                x[i] = pack2(f.x, f.y);
             }
+            const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+            top = fmaxf(f.x, f.y);
+        } else {
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = pack2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+            const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+            top = fmaxf(f.x, f.y);
         }
     }
 };
 
+// What a team of threads (a warp, or a CTA) shares.  Two of what the first warp may still read, or set, when the others are at the
+// next row.
+template <int NW, int LIST>
 struct LogShared {
-    Sums sums[kLogWarps];
-    Sums parts[kMaxLogCtas];                            // of the cluster's CTAs (in the first one's memory)
-    unsigned long long best[kMaxLogCtas * kMaxTop];     // their largest, in order
-    unsigned long long mine[kMaxTop];
-    unsigned long long list[kLogList];
-    unsigned bound[kLogWarps];
-    int count, votes[2];
+    uint4 named[kNamed / 4];
+    unsigned long long list[LIST];
+    unsigned long long mine[kMaxTop];                   // the largest, in order
+    Sums sums[2][NW];
+    int listed[2], reached[2], votes;
     float odd[16];                                      // values in front of the first whole 16 bytes and behind the last
+    unsigned short who[32 * NW];                        // threads whose largest reaches the bound
+};
+struct LogClusterShared {                               // (in the first CTA's memory)
+    Sums parts[kMaxLogCtas];
+    unsigned long long best[kMaxLogCtas * kMaxTop];
 };
 
 // Shared memory of the cluster's first CTA at the address of this CTA's `p`.
 __device__ __forceinline__ unsigned in_first_cta(const void* p) { return cluster_map(smem_u32(p), 0); }
 
-template <class T, bool CLUSTER>
-__global__ void __launch_bounds__(kLogThreads) token_logprobs_kernel(const LogArgs a)
-{
-    extern __shared__ __align__(16) unsigned char s_vals[];   // the part's whole 16 bytes
-    __shared__ LogShared sh;
-    constexpr int V = Vec<T>::N;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int ctas = CLUSTER ? (int)gridDim.x : 1, rank = CLUSTER ? (int)blockIdx.x : 0, r = CLUSTER ? (int)blockIdx.y : (int)blockIdx.x;
-    const int first = rank * a.part, n = max(0, min(a.part, a.vocab - first));
-    if (CLUSTER) cluster_arrive();
-    if (tid == 0) sh.count = 0;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const T* const whole_row = static_cast<const T*>(a.logits) + (long long)r * a.row_stride;
-    const T* const row = whole_row + first;
-    const int token = a.tokens && rank == 0 && tid == 0 ? (int)ld_global_u32(a.tokens + r) : -1;
-    const bool wanted = (unsigned)token < (unsigned)a.vocab;
-    const float chosen = wanted ? (float)whole_row[token] : 0.0f;
+// A row of a type's values from `first` on: the odd ones in front, whole 16 bytes, the odd ones behind.
+template <class T>
+struct LogPart {
+    static constexpr int V = Vec<T>::N;
+    const T* row;
+    int head, vecs, odd;
+    __device__ __forceinline__ LogPart(const T* p, int n) : row(p)
+    {
+        head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
+        vecs = (n - head) / V;
+        odd = n - vecs * V;
+    }
+    __device__ __forceinline__ int place_of_odd(int i) const { return i < head ? i : vecs * V + i; }
+    __device__ __forceinline__ const void* vec(int i) const { return row + head + (size_t)i * V; }
+};
 
-    // ---- one pass
-    Sums sum = {-INFINITY, 0.0f, 0.0f};
-    float largest = -INFINITY;          // (not-a-number is not seen here: the value is one that some value reaches; and it makes the sums not-a-number)
-    const bool entropy = a.entropy != nullptr;
-    auto add = [&](const float* x, auto count) {
-        constexpr int N = decltype(count)::value;
-        float m = x[0];
+constexpr int kVecs = 4;                // vectors of a thread on their way at a time
+
+// TEAM threads for a part: 32 (a warp of several in the CTA) or the whole CTA.
+template <class T, int TEAM, int LIST>
+struct LogTeam {
+    static constexpr int NW = TEAM / 32, V = Vec<T>::N;
+    LogShared<NW, LIST>& sh;
+    const LogArgs& a;
+    int tid, lane, warp;                // in the team
+    int turn;                           // 0, 1, 0, ... row after row
+    Sums sum;
+    float largest;                      // (not-a-number is not seen here: some value reaches it; and it makes the sums not-a-number)
+
+    static __device__ __forceinline__ void sync()
+    {
+        if constexpr (TEAM == 32) __syncwarp();
+        else __syncthreads();
+    }
+    __device__ __forceinline__ void load(uint4* w, const LogPart<T>& p, int i0) const
+    {
 #pragma unroll
-        for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+        for (int u = 0; u < kVecs; ++u) w[u] = ld_global_v4_if(i0 + u * TEAM < p.vecs, p.vec(i0 + u * TEAM));
+    }
+    // a new maximum, if it is one; what is subtracted
+    __device__ __forceinline__ float reach(float m)
+    {
         if (m > largest) {
             largest = m;
             move_to(sum, m);
         }
-        const float base = sum.m == -INFINITY ? 0.0f : sum.m;
-        float s = 0.0f, t = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float d = x[i] - base, e = exp_of(d);
-            s += e;
-            if (entropy) t = fmaf(e, fmaxf(d, -1e30f), t);      // (-infinity: 0, not 0 times infinity)
-        }
-        sum.s += s;
-        sum.t += t;
-    };
-    const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(T));
-    const int vecs = (n - head) / V, odd = n - vecs * V;        // odd ones: the head, then the tail; V - 1 of each at most
-    auto place_of_odd = [&](int i) { return i < head ? i : vecs * V + i; };
-    if (tid < odd) {
-        const float x = (float)row[place_of_odd(tid)];
-        sh.odd[tid] = x;
-        add(&x, std::integral_constant<int, 1>());
+        return sum.m == -INFINITY ? 0.0f : sum.m;
     }
-    constexpr int kU = 4;
-#pragma unroll 1
-    for (int i0 = tid; i0 < vecs; i0 += kLogThreads * kU) {
-        uint4 w[kU];
+    __device__ __forceinline__ void begin(const LogPart<T>& p)
+    {
+        sum = {-INFINITY, 0.0f, 0.0f};
+        largest = -INFINITY;
+        if (tid < p.odd) {
+            const float x = (float)p.row[p.place_of_odd(tid)];
+            sh.odd[tid] = x;
+            const float d = x - reach(x), e = exp_of(d);
+            sum.s += e;
+            sum.t = fmaf(e, fmaxf(d, -1e30f), sum.t);           // (-infinity: 0, not 0 times infinity)
+        }
+        if (tid == 0) sh.listed[turn] = sh.reached[turn] = 0;
+    }
+    __device__ __forceinline__ void add(const uint4* w, const LogPart<T>& p, int i0)
+    {
+        const bool entropy = a.entropy != nullptr;
+        float top = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) w[u] = ld_global_v4_if(i0 + u * kLogThreads < vecs, row + head + (size_t)(i0 + u * kLogThreads) * V);
+        for (int u = 0; u < kVecs; ++u)
+            if (i0 + u * TEAM < p.vecs) top = fmaxf(top, Vec<T>(w[u]).top);
+        const float base = reach(top);
+        unsigned long long s = 0ull, t = 0ull;
+        float lo, hi;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            const int i = i0 + u * kLogThreads;
-            if (i < vecs) {
-                if (a.keep) *reinterpret_cast<uint4*>(s_vals + (size_t)i * 16) = w[u];
+        for (int u = 0; u < kVecs; ++u)
+            if (i0 + u * TEAM < p.vecs) {
                 const Vec<T> v(w[u]);
-                add(v.x, std::integral_constant<int, V>());
+#pragma unroll
+                for (int i = 0; i < Vec<T>::P; ++i) {
+                    const unsigned long long d = fadd2(v.x[i], pack2(-base, -base));
+                    unpack2(fmul2(d, pack2(kLog2e, kLog2e)), lo, hi);
+                    const unsigned long long e = pack2(exp2_of(lo), exp2_of(hi));
+                    s = fadd2(s, e);
+                    if (entropy) ffma2(t, e, d);
+                }
+            }
+        unpack2(s, lo, hi);
+        sum.s += lo + hi;
+        unpack2(t, lo, hi);
+        float both = lo + hi;
+        if (both != both) {                                     // 0 times infinity, unless it is not-a-number in earnest
+            both = 0.0f;
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u)
+                if (i0 + u * TEAM < p.vecs) {
+                    const Vec<T> v(w[u]);
+#pragma unroll
+                    for (int i = 0; i < Vec<T>::P; ++i) {
+                        unpack2(v.x[i], lo, hi);
+                        both = fmaf(exp_of(lo - base), fmaxf(lo - base, -1e30f), both);
+                        both = fmaf(exp_of(hi - base), fmaxf(hi - base, -1e30f), both);
+                    }
+                }
+        }
+        sum.t += both;
+    }
+    __device__ __forceinline__ void put(unsigned long long k)
+    {
+        const int at = atomicAdd(&sh.listed[turn], 1);
+        if (at < LIST) sh.list[at] = k;
+    }
+    // The sums of the warps and, in order, the part's `top` largest keys (places within the part), for the first warp.
+    __device__ __forceinline__ void finish(const LogPart<T>& p)
+    {
+        constexpr int kEach = NW == 1 ? 0 : 32 / NW > 4 ? 32 / NW : 4;   // that a warp names at least
+        const int full = min(NW, p.vecs / 32);                  // warps all of whose threads have values
+        const int each = full == 0 ? 0 : max(kEach, (a.top + full - 1) / full);
+        unsigned least = 0u;
+        if (a.top > 0) {
+            unsigned mine = value_bits(largest);
+            unsigned* const named = reinterpret_cast<unsigned*>(sh.named);
+            for (int q = 0; q < each && warp < full; ++q) {
+                const unsigned best = __reduce_max_sync(0xffffffffu, mine);
+                const unsigned who = __ballot_sync(0xffffffffu, mine == best);
+                if (lane == __ffs(who) - 1) mine = 0u;
+                if (NW == 1) least = best;                      // (the last one stands)
+                else if (lane == 0) named[warp * each + q] = best;
+            }
+            if (NW > 1 && tid < kNamed && tid >= full * each) named[tid] = 0u;
+        }
+        const Sums all = joined(sum);
+        if (lane == 0) sh.sums[turn][warp] = all;
+        sync();
+        if (a.top == 0) return;
+        if (NW > 1) {                                           // the top-th of those named, by every warp for itself
+            constexpr int kTwo = NW * kEach > 32 ? 2 : 1;
+            const unsigned* const named = reinterpret_cast<const unsigned*>(sh.named);
+            if (full * each <= 32 * kTwo) {
+                unsigned v[kTwo];
+                int before[kTwo];
+#pragma unroll
+                for (int h = 0; h < kTwo; ++h) v[h] = named[h * 32 + lane], before[h] = 0;
+#pragma unroll
+                for (int j = 0; j < 8 * kTwo; ++j) {
+                    const uint4 o = sh.named[j];
+#pragma unroll
+                    for (int h = 0; h < kTwo; ++h) before[h] += (o.x > v[h]) + (o.y > v[h]) + (o.z > v[h]) + (o.w > v[h]);
+                }
+                // (of equal ones any: the least of those with fewer than `top` before them)
+#pragma unroll
+                for (int h = 0; h < kTwo; ++h) {
+                    const unsigned k = __reduce_min_sync(0xffffffffu, before[h] < a.top ? v[h] : 0xffffffffu);
+                    least = h == 0 ? k : min(least, k);
+                }
+            } else {                                            // few warps with values, which name up to 32 each: the least of all
+                least = 0xffffffffu;
+                for (int j = lane; j < full * each; j += 32) least = min(least, named[j]);
+                least = __reduce_min_sync(0xffffffffu, least);
             }
         }
-    }
-    Sums all = sum;
+        const float floor = least == 0u ? -INFINITY : value_of(least);
+        // the threads whose largest reaches the bound, or who have met not-a-number; their vectors, by all threads
+        if (value_bits(largest) >= least || sum.s != sum.s) sh.who[atomicAdd(&sh.reached[turn], 1)] = (unsigned short)tid;
+        sync();
+        const int shift = 32 - __clz(max(p.vecs - 1, 0) / TEAM), pairs = sh.reached[turn] << shift;   // (2^shift: vectors of a thread, or more)
+        for (int x = tid; x < pairs; x += TEAM) {
+            const int i = sh.who[x >> shift] + (x & ((1 << shift) - 1)) * TEAM;
+            if (i >= p.vecs) continue;
+            const Vec<T> v(ld_global_v4(p.vec(i)));
+            float lo, hi, any = 0.0f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) all = joined(all, shuffled(all, o));
-    if (lane == 0) sh.sums[warp] = all;
-
-    // ---- the largest values
-    if (a.top > 0) {
-        const int full = min(kLogWarps, vecs / 32);            // warps all of whose threads have values
-        unsigned mine = value_bits(largest), bound = 0u;
-        if (warp < full)
-            for (int q = (a.top + full - 1) / full; q > 0; --q) {
-                bound = __reduce_max_sync(0xffffffffu, mine);
-                const unsigned who = __ballot_sync(0xffffffffu, mine == bound);
-                if (lane == __ffs(who) - 1) mine = 0u;
+            for (int e = 0; e < Vec<T>::P; ++e) {
+                unpack2(v.x[e], lo, hi);
+                any += lo + hi;                                 // (not-a-number if one of them is)
             }
-        if (lane == 0) sh.bound[warp] = warp < full ? bound : 0xffffffffu;
-        __syncthreads();
-        unsigned least = full == 0 || full * 32 < a.top ? 0u : sh.bound[lane % kLogWarps];
-        least = __reduce_min_sync(0xffffffffu, least);
-        // each value of the part with its place; `f` is called by all threads the same number of times
-        auto each = [&](auto f) {
-            if (tid < odd) f(key_of(sh.odd[tid], place_of_odd(tid)));
+            if (v.top >= floor || any != any) {
+#pragma unroll
+                for (int e = 0; e < Vec<T>::P; ++e) {
+                    unpack2(v.x[e], lo, hi);
+                    if (!(lo < floor)) put(key_of(lo, p.head + i * V + 2 * e));
+                    if (!(hi < floor)) put(key_of(hi, p.head + i * V + 2 * e + 1));
+                }
+            }
+        }
+        if (tid < p.odd && !(sh.odd[tid] < floor)) put(key_of(sh.odd[tid], p.place_of_odd(tid)));
+        sync();
+        int listed = sh.listed[turn];
+        if (listed > LIST) {                                    // the top-th largest key, bit by bit
+            // each value of the part with its place
+            auto each_key = [&](auto f) {
+                if (tid < p.odd) f(key_of(sh.odd[tid], p.place_of_odd(tid)));
 #pragma unroll 1
-            for (int i = tid; i < vecs; i += kLogThreads) {
-                const uint4 w = a.keep ? *reinterpret_cast<const uint4*>(s_vals + (size_t)i * 16) : ld_global_v4(row + head + (size_t)i * V);
-                const Vec<T> v(w);
-#pragma unroll
-                for (int e = 0; e < V; ++e) f(key_of(v.x[e], head + i * V + e));
-            }
-        };
-        unsigned long long from = (unsigned long long)least << 32;
-        each([&](unsigned long long k) {
-            if (k >= from) {
-                const int at = atomicAdd(&sh.count, 1);
-                if (at < kLogList) sh.list[at] = k;
-            }
-        });
-        __syncthreads();
-        int listed = sh.count;
-        if (listed > kLogList) {                                // the top-th largest key, bit by bit
-            from = 0ull;
+                for (int i = tid; i < p.vecs * V; i += TEAM) f(key_of((float)p.row[p.head + i], p.head + i));
+            };
+            unsigned long long from = 0ull;
 #pragma unroll 1
             for (int bit = 63; bit >= 0; --bit) {
                 const unsigned long long trial = from | 1ull << bit;
                 int c = 0;
-                each([&](unsigned long long k) { c += k >= trial; });
+                each_key([&](unsigned long long k) { c += k >= trial; });
                 c = __reduce_add_sync(0xffffffffu, c);
-                if (tid < 2) sh.votes[tid] = 0;
-                __syncthreads();
-                if (lane == 0) atomicAdd(&sh.votes[0], c);
-                __syncthreads();
-                if (sh.votes[0] >= a.top) from = trial;
-                __syncthreads();
+                sync();
+                if (tid == 0) sh.votes = 0;
+                sync();
+                if (lane == 0) atomicAdd(&sh.votes, c);
+                sync();
+                if (sh.votes >= a.top) from = trial;
             }
-            if (tid == 0) sh.count = 0;
-            __syncthreads();
-            each([&](unsigned long long k) {
-                if (k >= from) sh.list[atomicAdd(&sh.count, 1)] = k;    // (keys are distinct: these are `top`, or all of the part)
+            sync();
+            if (tid == 0) sh.listed[turn] = 0;
+            sync();
+            each_key([&](unsigned long long k) {
+                if (k >= from) put(k);                          // (keys are distinct: these are `top`, or all of the part)
             });
-            __syncthreads();
-            listed = sh.count;
+            sync();
+            listed = sh.listed[turn];
         }
-        if (tid < a.top) sh.mine[tid] = 0ull;                   // (a part may have fewer)
-        __syncthreads();
-        for (int i = tid; i < listed; i += kLogThreads) {
+        const bool many = NW > 1 && listed > 128;               // then all threads look for the places, else the first warp alone
+        if (warp > 0 && !many) return;
+        if (tid < a.top && listed < a.top) sh.mine[tid] = 0ull;
+        if (many) sync();
+        else __syncwarp();
+        for (int i = tid; i < listed; i += many ? TEAM : 32) {
             const unsigned long long k = sh.list[i];
             int before = 0;
             for (int j = 0; j < listed; ++j) before += sh.list[j] > k;
             if (before < a.top) sh.mine[before] = k;
         }
+        if (many) sync();
+        else __syncwarp();
     }
-    __syncthreads();
-    Sums part = sh.sums[lane % kLogWarps];
-#pragma unroll
-    for (int o = kLogWarps / 2; o > 0; o >>= 1) part = joined(part, shuffled(part, o));
+    __device__ __forceinline__ Sums all_sums() const { return joined(lane < NW ? sh.sums[turn][lane] : Sums{-INFINITY, 0.0f, 0.0f}); }
+};
 
-    // ---- the parts of a row, in the cluster's first CTA
-    if (CLUSTER) {
-        cluster_wait();                                         // (all CTAs have begun)
-        if (warp == 0) {
-            if (lane == 0) {
-                const unsigned to = in_first_cta(&sh.parts[rank]);
-                asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;" ::"r"(to),
-                             "f"(part.m), "f"(part.s), "f"(part.t)
-                             : "memory");
-            }
-            if (lane < a.top) {
-                const unsigned long long k = sh.mine[lane];     // (places of the whole row)
-                const unsigned long long whole = k == 0ull ? 0ull : k - (unsigned)first;
-                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_first_cta(&sh.best[rank * a.top + lane])), "l"(whole) : "memory");
-            }
-        }
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        if (rank != 0) return;
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        part = lane < ctas ? sh.parts[lane] : Sums{-INFINITY, 0.0f, 0.0f};
+// The row's answers from its sums, by the threads that have a key or are the first.
+struct LogAnswer {
+    const LogArgs& a;
+    size_t r;
+    float m, logsum, mean;
+    bool none;
+    __device__ __forceinline__ LogAnswer(const LogArgs& args, size_t row, const Sums& x)
+        : a(args), r(row), m(x.m), logsum(logf(x.s)), mean(x.t / x.s),
+          none(!(fabsf(x.m) < INFINITY) || x.s != x.s)          // (a row of -infinity alone, or with not-a-number or +infinity)
+    {
+    }
+    static __device__ __forceinline__ float nan() { return __int_as_float(0x7fffffff); }
+    __device__ __forceinline__ void scalars(bool wanted, float chosen) const
+    {
+        if (a.logprob) a.logprob[r] = none || !wanted ? nan() : (chosen - m) - logsum;
+        if (a.entropy) a.entropy[r] = none ? nan() : logsum - mean;
+    }
+    __device__ __forceinline__ void place(int i, unsigned long long k) const
+    {
+        a.top_index[r * a.top + i] = place_of(k);
+        a.top_logprob[r * a.top + i] = none ? nan() : (value_of((unsigned)(k >> 32)) - m) - logsum;
+    }
+};
+
+// Rows one after the other, a team of threads each: the values of the next 4 vectors of a thread, be they of the next row, are on
+// their way while those before are added or the row is finished.
+template <class T, int TEAM>
+__global__ void __launch_bounds__(256, 4) token_logprobs_rows_kernel(const LogArgs a, int rows)
+{
+    constexpr int kTeams = 256 / TEAM, kList = TEAM == 32 ? 256 : kLogList;
+    __shared__ LogShared<TEAM / 32, kList> shared[kTeams];
+    const int which = threadIdx.x / TEAM, tid = threadIdx.x % TEAM;
+    LogTeam<T, TEAM, kList> team = {shared[which], a, tid, (int)threadIdx.x & 31, tid >> 5, 0, {}, 0.0f};
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const T* const logits = static_cast<const T*>(a.logits);
+    uint4 w[kVecs];
+    int r = blockIdx.x * kTeams + which;
+    const int step = gridDim.x * kTeams;
+    if (r < rows) team.load(w, LogPart<T>(logits + (long long)r * a.row_stride, a.vocab), tid);
+    for (; r < rows; r += step) {
+        const LogPart<T> part(logits + (long long)r * a.row_stride, a.vocab);
+        const int token = a.tokens && tid == 0 ? (int)ld_global_u32(a.tokens + r) : -1;
+        const bool wanted = (unsigned)token < (unsigned)a.vocab;
+        const float chosen = wanted ? (float)part.row[token] : 0.0f;
+        team.begin(part);
+        for (int i0 = 0; i0 == 0 || i0 < part.vecs; i0 += TEAM * kVecs) {
+            uint4 next[kVecs];
+            if (i0 + TEAM * kVecs < part.vecs) team.load(next, part, i0 + TEAM * kVecs + tid);
+            else if (r + step < rows) team.load(next, LogPart<T>(logits + (long long)(r + step) * a.row_stride, a.vocab), tid);
+            team.add(w, part, i0 + tid);
 #pragma unroll
-        for (int o = kMaxLogCtas / 2; o > 0; o >>= 1) part = joined(part, shuffled(part, o));
-    }
-    // (of a row without a finite value m is infinite: not-a-number.  In a row of the cluster the lanes from 8 on have joined nothing)
-    const float m = __shfl_sync(0xffffffffu, part.m, 0), s = __shfl_sync(0xffffffffu, part.s, 0), t = __shfl_sync(0xffffffffu, part.t, 0);
-    const bool none = !(fabsf(m) < INFINITY) || s != s;
-    const float nan = __int_as_float(0x7fffffff), logsum = logf(s);
-    if (tid == 0) {
-        if (a.logprob) a.logprob[r] = none || !wanted ? nan : (chosen - m) - logsum;
-        if (a.entropy) a.entropy[r] = none ? nan : logsum - t / s;
-    }
-    auto put = [&](int i, unsigned long long k) {
-        a.top_index[(size_t)r * a.top + i] = place_of(k);
-        a.top_logprob[(size_t)r * a.top + i] = none ? nan : (value_of((unsigned)(k >> 32)) - m) - logsum;
-    };
-    if (!CLUSTER) {
-        if (tid < a.top) put(tid, sh.mine[tid]);
-    } else {
-        const int keys = ctas * a.top;
-        if (tid < keys) {
-            const unsigned long long k = sh.best[tid];
-            int before = 0;
-            for (int j = 0; j < keys; ++j) before += sh.best[j] > k;
-            if (k != 0ull && before < a.top) put(before, k);
+            for (int u = 0; u < kVecs; ++u) w[u] = next[u];
         }
+        team.finish(part);
+        if (team.warp == 0) {
+            const LogAnswer answer(a, r, team.all_sums());
+            if (tid == 0) answer.scalars(wanted, chosen);
+            if (tid < a.top) answer.place(tid, team.sh.mine[tid]);
+            __syncwarp();
+        }
+        team.turn ^= 1;
+    }
+}
+
+// A row for the CTAs of a cluster, a part each, which meet in the first one.
+constexpr int kPartThreads = 512;
+template <class T>
+__global__ void __launch_bounds__(kPartThreads, 2) token_logprobs_parts_kernel(const LogArgs a)
+{
+    __shared__ LogShared<kPartThreads / 32, kLogList> shared;
+    __shared__ LogClusterShared meet;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    LogTeam<T, kPartThreads, kLogList> team = {shared, a, tid, lane, warp, 0, {}, 0.0f};
+    const int ctas = (int)gridDim.x, rank = (int)blockIdx.x, r = (int)blockIdx.y;
+    const int first = rank * a.part, n = max(0, min(a.part, a.vocab - first));
+    cluster_arrive();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const T* const row = static_cast<const T*>(a.logits) + (long long)r * a.row_stride;
+    const int token = a.tokens && rank == 0 && tid == 0 ? (int)ld_global_u32(a.tokens + r) : -1;
+    const LogPart<T> part(row + first, n);
+    uint4 w[kVecs];
+    team.load(w, part, tid);
+    team.begin(part);
+    for (int i0 = 0; i0 < part.vecs;) {
+        team.add(w, part, i0 + tid);
+        i0 += kPartThreads * kVecs;
+        if (i0 < part.vecs) team.load(w, part, i0 + tid);
+    }
+    const bool wanted = (unsigned)token < (unsigned)a.vocab;
+    const float chosen = wanted ? (float)row[token] : 0.0f;
+    team.finish(part);
+    cluster_wait();                                             // (all CTAs have begun)
+    if (warp == 0) {
+        const Sums mine = team.all_sums();
+        if (lane == 0) {
+            const unsigned to = in_first_cta(&meet.parts[rank]);
+            asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;" ::"r"(to), "f"(mine.m),
+                         "f"(mine.s), "f"(mine.t)
+                         : "memory");
+        }
+        if (lane < a.top) {
+            const unsigned long long k = shared.mine[lane];     // (places of the whole row)
+            const unsigned long long whole = k == 0ull ? 0ull : k - (unsigned)first;
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_first_cta(&meet.best[rank * a.top + lane])), "l"(whole) : "memory");
+        }
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (rank != 0) return;                                      // (the first CTA stays until all have sent)
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const LogAnswer answer(a, r, joined(lane < ctas ? meet.parts[lane] : Sums{-INFINITY, 0.0f, 0.0f}));
+    if (tid == 0) answer.scalars(wanted, chosen);
+    const int keys = ctas * a.top;
+    if (tid < keys) {
+        const unsigned long long k = meet.best[tid];
+        int before = 0;
+        for (int j = 0; j < keys; ++j) before += meet.best[j] > k;
+        if (k != 0ull && before < a.top) answer.place(before, k);
     }
 }
 
 template <class T>
 cudaError_t launch_logprobs(LogArgs a, int rows, cudaStream_t s)
 {
-    // CTAs per row: enough for a part to stay in shared memory; more while there are fewer CTAs than two per SM and a thread would
-    // still have a vector of each part.
     const int sms = sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
     constexpr int V = Vec<T>::N;
+    // CTAs per row: more while there are fewer CTAs than two per SM and a thread would still have a vector of each part.
     int ctas = 1;
     auto part_of = [&](int c) { return ((a.vocab + c - 1) / c + V - 1) / V * V; };
-    while (ctas < kMaxLogCtas && ((size_t)part_of(ctas) * sizeof(T) > kLogKeep || ((long long)rows * ctas < 2 * sms && part_of(2 * ctas) >= kLogThreads * V))) ctas *= 2;
-    a.part = part_of(ctas);
-    const size_t bytes = (size_t)a.part * sizeof(T);
-    a.keep = a.top > 0 && bytes <= kLogKeep;
-    const size_t smem = a.keep ? bytes : 0;
-    static thread_local int allowed_dev = -1;
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess) return err;
-    if (allowed_dev != dev) {
-        err = cudaFuncSetAttribute(token_logprobs_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLogKeep);
-        if (err == cudaSuccess) err = cudaFuncSetAttribute(token_logprobs_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLogKeep);
-        if (err != cudaSuccess) return err;
-        allowed_dev = dev;
+    while (ctas < kMaxLogCtas && (long long)rows * ctas < 2 * sms && part_of(2 * ctas) >= kPartThreads * V) ctas *= 2;
+    if (ctas == 1) {
+        if (a.vocab <= kWarpVocab) {
+            const int teams = (rows + 7) / 8;
+            return launch_overlapping(token_logprobs_rows_kernel<T, 32>, dim3(teams < 4 * sms ? teams : 4 * sms), 256, 0, s, a, rows);
+        }
+        return launch_overlapping(token_logprobs_rows_kernel<T, 256>, dim3(rows < 4 * sms ? rows : 4 * sms), 256, 0, s, a, rows);
     }
+    a.part = part_of(ctas);
     cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(kLogThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.blockDim = dim3(kPartThreads);
+    cfg.gridDim = dim3(ctas, rows);                             // (fewer rows than two per SM)
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -343,26 +522,9 @@ cudaError_t launch_logprobs(LogArgs a, int rows, cudaStream_t s)
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = g_no_pdl ? attr + 1 : attr;
-    cfg.numAttrs = (g_no_pdl ? 0 : 1) + (ctas > 1 ? 1 : 0);
-    if (ctas == 1) {
-        cfg.gridDim = dim3(rows);
-        err = cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, false>, a);
-        if (err == cudaSuccess) count_launch();
-        return err;
-    }
-    // (rows are the grid's second dimension: 65535 at a time)
-    for (int r0 = 0; r0 < rows && err == cudaSuccess; r0 += 65535) {
-        const int some = rows - r0 < 65535 ? rows - r0 : 65535;
-        LogArgs b = a;
-        b.logits = static_cast<const T*>(a.logits) + (long long)r0 * a.row_stride;
-        if (a.tokens) b.tokens = a.tokens + r0;
-        if (a.logprob) b.logprob = a.logprob + r0;
-        if (a.entropy) b.entropy = a.entropy + r0;
-        if (a.top > 0) b.top_logprob = a.top_logprob + (size_t)r0 * a.top, b.top_index = a.top_index + (size_t)r0 * a.top;
-        cfg.gridDim = dim3(ctas, some);
-        err = cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, true>, b);
-        if (err == cudaSuccess) count_launch();
-    }
+    cfg.numAttrs = g_no_pdl ? 1 : 2;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, token_logprobs_parts_kernel<T>, a);
+    if (err == cudaSuccess) count_launch();
     return err;
 }
 
@@ -380,7 +542,7 @@ extern "C" spqt_status spqt_token_logprobs(const void* logits, int dtype, int ro
     const size_t size = dtype == SPQT_LOGITS_FP32 ? 4 : 2;
     if (!aligned(logits, size) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(top_logprob, 4) || !aligned(top_index, 4))
         return SPQT_ERR_ALIGNMENT;
-    const LogArgs a = {logits, row_stride, tokens, logprob, entropy, top_logprob, top_index, vocab, top, 0, 0};
+    const LogArgs a = {logits, row_stride, tokens, logprob, entropy, top_logprob, top_index, vocab, top, 0};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return launched(dtype == SPQT_LOGITS_FP16   ? launch_logprobs<__half>(a, rows, s)
                     : dtype == SPQT_LOGITS_BF16 ? launch_logprobs<__nv_bfloat16>(a, rows, s)
