@@ -660,7 +660,7 @@ __device__ __forceinline__ float2 joined(const float2* ml, int rows, int seg, in
     return make_float2(m, l);
 }
 
-constexpr int kJoinWarps = 4;
+constexpr int kJoinWarps = 4, kTilesAhead = 4;
 
 // CTAs below `rows_ctas`: one row of one segment each, its parts' sums added in the order of the CTAs (by four warps, then the
 // four).  The others: an equal part of all tiles each, a lane per token.
@@ -751,26 +751,49 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(cons
                 if (lane == 0) s_ml[r] = make_float2(v.x == -INFINITY ? 0.0f : v.x - kUp, v.y == 0.0f ? 0.0f : 1.0f / v.y);
             }
             __syncthreads();
-            for (int x = t + warp; x < stop; x += kJoinWarps) {
-                const int local = x - first;
-                const bool codes = local < nt;
-                const int token = (codes ? local * kTile : full + (local - nt) * 16) + lane;
-                if (token >= (codes ? full : n) || (!codes && lane >= 16)) continue;
-                const unsigned block = (unsigned)row[token >> shift];
-                if (block >= (unsigned)c.blocks) {
-                    refuse(a.status);
-                    continue;
-                }
-                float sum = 0.0f;
-                for (int r = 0; r < rows; r += 4) {
-                    const int rg = (rb + r) / ROWS;
-                    const float4 s = *reinterpret_cast<const float4*>(a.scores + ((size_t)(begin + rg * tiles + local) * kTile + lane) * ROWS + (rb + r) % ROWS);
-                    const float e[4] = {s.x, s.y, s.z, s.w};
+            // four tiles of a warp at a time: block numbers and scores, then the weights, are on their way together
+            for (int x0 = t + warp; x0 < stop; x0 += kJoinWarps * kTilesAhead) {
+                float sum[kTilesAhead];
+                float* to[kTilesAhead];
+                unsigned block[kTilesAhead];
+                int token[kTilesAhead];
+                bool there[kTilesAhead];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (r + k < rows) sum = fmaf(exp2_fast(e[k] - s_ml[r + k].x), s_ml[r + k].y, sum);
+                for (int u = 0; u < kTilesAhead; ++u) {
+                    const int x = x0 + u * kJoinWarps, local = x - first;
+                    const bool codes = local < nt;
+                    token[u] = (codes ? local * kTile : full + (local - nt) * 16) + lane;
+                    there[u] = x < stop && token[u] < (codes ? full : n) && (codes || lane < 16);
+                    block[u] = there[u] ? (unsigned)row[token[u] >> shift] : 0u;
+                    sum[u] = 0.0f;
                 }
-                c.weight[((size_t)block << shift) + (token & ((1 << shift) - 1))] += sum;
+                for (int r = 0; r < rows; r += 4) {
+                    const float* const from = a.scores + ((size_t)(begin + (rb + r) / ROWS * tiles + (x0 - first)) * kTile + lane) * ROWS + (rb + r) % ROWS;
+                    float4 s[kTilesAhead];
+#pragma unroll
+                    for (int u = 0; u < kTilesAhead; ++u)
+                        s[u] = there[u] ? *reinterpret_cast<const float4*>(from + u * (kJoinWarps * kTile * ROWS)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int u = 0; u < kTilesAhead; ++u) {
+                        const float e[4] = {s[u].x, s[u].y, s[u].z, s[u].w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (r + k < rows) sum[u] = fmaf(exp2_fast(e[k] - s_ml[r + k].x), s_ml[r + k].y, sum[u]);
+                    }
+                }
+                float old[kTilesAhead];
+#pragma unroll
+                for (int u = 0; u < kTilesAhead; ++u) {
+                    if (there[u] && block[u] >= (unsigned)c.blocks) {
+                        refuse(a.status);
+                        there[u] = false;
+                    }
+                    to[u] = c.weight + ((size_t)block[u] << shift) + (token[u] & ((1 << shift) - 1));
+                    old[u] = there[u] ? *to[u] : 0.0f;
+                }
+#pragma unroll
+                for (int u = 0; u < kTilesAhead; ++u)
+                    if (there[u]) *to[u] = old[u] + sum[u];
             }
         }
         t = stop;

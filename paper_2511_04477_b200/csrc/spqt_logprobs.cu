@@ -24,7 +24,6 @@ constexpr int kMaxTop = 32, kMaxVocab = 1 << 20;
 constexpr int kMaxLogCtas = 8;          // of a cluster
 constexpr int kNamed = 64;              // maxima that the warps name: 4 of each, or more of fewer warps
 constexpr int kLogList = 1536;          // values that may reach the bound
-constexpr int kWarpVocab = 4096;        // rows up to which a warp does one alone
 
 struct LogArgs {
     const void* logits;
@@ -86,34 +85,54 @@ __device__ __forceinline__ Sums joined(Sums a)
     return a;
 }
 
-// 16 bytes of values: two fp32 values in a register pair each, and their largest (not-a-number left out).
+// x - base in fp32 of two values of a word (exact where it counts: x near base)
+__device__ __forceinline__ unsigned long long less_base(unsigned w, float base, __half)
+{
+    float lo, hi;
+    asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.f16 %0, a, %3;\n\tadd.rn.f32.f16 %1, b, %3;\n\t}" : "=f"(lo), "=f"(hi) : "r"(w), "f"(-base));
+    return pack2(lo, hi);
+}
+__device__ __forceinline__ unsigned long long less_base(unsigned w, float base, __nv_bfloat16)
+{
+    return fadd2(pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)), pack2(-base, -base));
+}
+
+// 16 bytes of values.
 template <class T>
 struct Vec {
-    static constexpr int N = 16 / (int)sizeof(T), P = N / 2;
-    unsigned long long x[P];
-    float top;
-    __device__ __forceinline__ explicit Vec(const uint4& w)
+    static constexpr int N = 16 / (int)sizeof(T), P = N / 2;   // P pairs
+    uint4 w;
+    __device__ __forceinline__ explicit Vec(const uint4& v) : w(v) {}
+    __device__ __forceinline__ unsigned word(int i) const { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
+    __device__ __forceinline__ void pair(int i, float& lo, float& hi) const
     {
-        const unsigned u[4] = {w.x, w.y, w.z, w.w};
         if constexpr (sizeof(T) == 4) {
-            x[0] = pack2(__uint_as_float(u[0]), __uint_as_float(u[1]));
-            x[1] = pack2(__uint_as_float(u[2]), __uint_as_float(u[3]));
-            top = fmaxf(fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])), fmaxf(__uint_as_float(u[2]), __uint_as_float(u[3])));
+            lo = __uint_as_float(word(2 * i)), hi = __uint_as_float(word(2 * i + 1));
         } else if constexpr (std::is_same<T, __half>::value) {
-            const __half2* h = reinterpret_cast<const __half2*>(u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = __half22float2(h[i]);
-                x[i] = pack2(f.x, f.y);
-            }
-            const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-            top = fmaxf(f.x, f.y);
+            const unsigned u = word(i);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
+            lo = f.x, hi = f.y;
         } else {
-            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = pack2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+            lo = __uint_as_float(word(i) << 16), hi = __uint_as_float(word(i) & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ unsigned long long less(int i, float base) const
+    {
+        if constexpr (sizeof(T) == 4) return fadd2(pack2(__uint_as_float(word(2 * i)), __uint_as_float(word(2 * i + 1))), pack2(-base, -base));
+        else return less_base(word(i), base, T());
+    }
+    __device__ __forceinline__ float top() const               // the largest, not-a-number left out
+    {
+        if constexpr (sizeof(T) == 4) {
+            return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const __half2* h = reinterpret_cast<const __half2*>(&w);
+            const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+            return fmaxf(f.x, f.y);
+        } else {
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
             const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-            top = fmaxf(f.x, f.y);
+            return fmaxf(f.x, f.y);
         }
     }
 };
@@ -156,7 +175,7 @@ struct LogPart {
 
 constexpr int kVecs = 4;                // vectors of a thread on their way at a time
 
-// TEAM threads for a part: 32 (a warp of several in the CTA) or the whole CTA.
+// TEAM threads for a part: 32 or 128 (several teams in the CTA) or the whole CTA.
 template <class T, int TEAM, int LIST>
 struct LogTeam {
     static constexpr int NW = TEAM / 32, V = Vec<T>::N;
@@ -170,6 +189,7 @@ struct LogTeam {
     static __device__ __forceinline__ void sync()
     {
         if constexpr (TEAM == 32) __syncwarp();
+        else if constexpr (TEAM == 128) asm volatile("bar.sync %0, 128;" ::"r"((int)threadIdx.x / 128 + 1) : "memory");
         else __syncthreads();
     }
     __device__ __forceinline__ void load(uint4* w, const LogPart<T>& p, int i0) const
@@ -205,7 +225,7 @@ struct LogTeam {
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kVecs; ++u)
-            if (i0 + u * TEAM < p.vecs) top = fmaxf(top, Vec<T>(w[u]).top);
+            if (i0 + u * TEAM < p.vecs) top = fmaxf(top, Vec<T>(w[u]).top());
         const float base = reach(top);
         unsigned long long s = 0ull, t = 0ull;
         float lo, hi;
@@ -215,7 +235,7 @@ struct LogTeam {
                 const Vec<T> v(w[u]);
 #pragma unroll
                 for (int i = 0; i < Vec<T>::P; ++i) {
-                    const unsigned long long d = fadd2(v.x[i], pack2(-base, -base));
+                    const unsigned long long d = v.less(i, base);
                     unpack2(fmul2(d, pack2(kLog2e, kLog2e)), lo, hi);
                     const unsigned long long e = pack2(exp2_of(lo), exp2_of(hi));
                     s = fadd2(s, e);
@@ -234,7 +254,7 @@ struct LogTeam {
                     const Vec<T> v(w[u]);
 #pragma unroll
                     for (int i = 0; i < Vec<T>::P; ++i) {
-                        unpack2(v.x[i], lo, hi);
+                        v.pair(i, lo, hi);
                         both = fmaf(exp_of(lo - base), fmaxf(lo - base, -1e30f), both);
                         both = fmaf(exp_of(hi - base), fmaxf(hi - base, -1e30f), both);
                     }
@@ -308,13 +328,13 @@ struct LogTeam {
             float lo, hi, any = 0.0f;
 #pragma unroll
             for (int e = 0; e < Vec<T>::P; ++e) {
-                unpack2(v.x[e], lo, hi);
+                v.pair(e, lo, hi);
                 any += lo + hi;                                 // (not-a-number if one of them is)
             }
-            if (v.top >= floor || any != any) {
+            if (v.top() >= floor || any != any) {
 #pragma unroll
                 for (int e = 0; e < Vec<T>::P; ++e) {
-                    unpack2(v.x[e], lo, hi);
+                    v.pair(e, lo, hi);
                     if (!(lo < floor)) put(key_of(lo, p.head + i * V + 2 * e));
                     if (!(hi < floor)) put(key_of(hi, p.head + i * V + 2 * e + 1));
                 }
@@ -399,7 +419,7 @@ struct LogAnswer {
 template <class T, int TEAM>
 __global__ void __launch_bounds__(256, 4) token_logprobs_rows_kernel(const LogArgs a, int rows)
 {
-    constexpr int kTeams = 256 / TEAM, kList = TEAM == 32 ? 256 : kLogList;
+    constexpr int kTeams = 256 / TEAM, kList = TEAM == 32 ? 256 : TEAM == 128 ? 1024 : kLogList;
     __shared__ LogShared<TEAM / 32, kList> shared[kTeams];
     const int which = threadIdx.x / TEAM, tid = threadIdx.x % TEAM;
     LogTeam<T, TEAM, kList> team = {shared[which], a, tid, (int)threadIdx.x & 31, tid >> 5, 0, {}, 0.0f};
@@ -503,11 +523,15 @@ cudaError_t launch_logprobs(LogArgs a, int rows, cudaStream_t s)
     auto part_of = [&](int c) { return ((a.vocab + c - 1) / c + V - 1) / V * V; };
     while (ctas < kMaxLogCtas && (long long)rows * ctas < 2 * sms && part_of(2 * ctas) >= kPartThreads * V) ctas *= 2;
     if (ctas == 1) {
-        if (a.vocab <= kWarpVocab) {
-            const int teams = (rows + 7) / 8;
-            return launch_overlapping(token_logprobs_rows_kernel<T, 32>, dim3(teams < 4 * sms ? teams : 4 * sms), 256, 0, s, a, rows);
-        }
-        return launch_overlapping(token_logprobs_rows_kernel<T, 256>, dim3(rows < 4 * sms ? rows : 4 * sms), 256, 0, s, a, rows);
+        auto rows_by = [&](auto kernel, int team) {
+            const int teams = 256 / team, grid = (rows + teams - 1) / teams;
+            return launch_overlapping(kernel, dim3(grid < 4 * sms ? grid : 4 * sms), 256, 0, s, a, rows);
+        };
+        // 2000 x 8000 fp16, top 20, a warp / 128 threads a row: 24.3 / 19.3 us; 4096 x 8000: 22.4 / 31.1; 1000 x 2000: 5.7 / 7.0; 1000 x 4000: 13.5 / 8.1.
+        // 128 / 256 threads: 2048 x 32000 42.5 / 44.7; 512 x 128256 48.8 / 37.1
+        if (a.vocab <= 2048 || (a.vocab <= 8192 && rows >= 16 * sms)) return rows_by(token_logprobs_rows_kernel<T, 32>, 32);
+        if ((size_t)a.vocab * sizeof(T) <= 65536) return rows_by(token_logprobs_rows_kernel<T, 128>, 128);
+        return rows_by(token_logprobs_rows_kernel<T, 256>, 256);
     }
     a.part = part_of(ctas);
     cudaLaunchConfig_t cfg = {};
