@@ -16,10 +16,11 @@
 // the columns that they leave free, else in a second instruction.  Without it the result is 1.4 times as far from the exact one,
 // as far as its own rounding to fp16 takes it.  Sums are fp32 and know nothing of v's scales.
 //
-// Work: the tiles (32 tokens) of all streams are laid end to end and cut into equal parts, one per CTA; the warps of a CTA take its
-// tiles in turn, each with a ring of tiles on their way (cp.async, so that a block number is all that is needed ahead).  A stream
-// that lies within one CTA is finished there; the others' parts meet in a second kernel, which adds them in the order of the CTAs
-// and, where asked, turns the scores that the first one left into probabilities and adds them to the tokens' weights.
+// Work: the tiles (32 tokens) of all segments (a stream, or sixteen of its rows where it has more) are laid end to end, each
+// segment with some room in front for what it costs beside its tiles, and cut into equal parts, one per CTA; the warps of a CTA take
+// its tiles in turn, each with a ring of tiles on their way (cp.async, so that a block number is all that is needed ahead).  A segment
+// that lies within one CTA is finished there; of the others the CTA that comes last adds the parts, in the order of the CTAs.  Where
+// weights are accumulated, a second kernel turns the scores that the first one left into probabilities.
 #include <cuda_fp8.h>
 
 #include "spqt_common.cuh"
@@ -30,6 +31,7 @@
 namespace spqt {
 
 constexpr int kTile = 32;               // tokens of a tile of codes; half as many of the block that is not full
+constexpr int kRoom = 12;               // tiles that a segment costs beside its own (131072 tokens, eight streams: FIXROOM)
 constexpr int kMaxAttnCtas = 320;       // parts at most
 constexpr int kLengthCache = 1024;      // streams whose lengths a CTA keeps in shared memory
 constexpr float kUp = 10.0f;            // p of the largest score is 2^kUp, when M is set
@@ -47,10 +49,13 @@ struct AttnArgs {
     int accumulate;
     float scale_log2;
     int* status;
-    int* begin;                         // workspace: the first tile of every segment (a stream's row group), behind them their sum
+    int* begin;                         // workspace: the place of every segment's first tile, behind them the sum of tiles and rooms
+    int* arrived;                       // parts that are there, of every segment; zero between calls
     float2* ml;                         // parts: (M, l) of every row
     float* o;                           // parts: sums of every row, not divided yet
-    float* scores;                      // tiles: [kTile][ROWS], in powers of two
+    float2* lse;                        // segments: M - kUp and 1 / l of every row
+    int4* tiles;                        // places: what tile it is, see TileNote
+    float* scores;                      // places: [kTile][ROWS], in powers of two
 };
 
 template <int D, int ROWS>
@@ -67,13 +72,19 @@ __device__ __forceinline__ int full_tokens(int n, int shift) { return n >> shift
 __device__ __forceinline__ int code_tiles(int n, int shift) { return (full_tokens(n, shift) + kTile - 1) / kTile; }
 __device__ __forceinline__ int tiles_of(int n, int shift) { return code_tiles(n, shift) + (n - full_tokens(n, shift) + 15) / 16; }
 
-// CTAs that work: not more than leave a tile for every warp, unless there are more segments.  A CTA's tiles begin at
-// total * i / ctas.
-__device__ __forceinline__ int working_ctas(int total, int segments, int warps, int most)
+__device__ __forceinline__ int places_of(int tiles) { return tiles == 0 ? 0 : kRoom + tiles; }
+
+// CTAs that work: not more than leave a tile for every warp.  A CTA's places begin at total * i / ctas.  (In fp64: the products
+// are exact, and a quotient that is no whole number is 1/ctas or more from one.)
+__device__ __forceinline__ int working_ctas(int total, int warps, int most) { return min(max((total + warps - 1) / warps, 1), most); }
+__device__ __forceinline__ int begin_of(int cta, int total, int ctas) { return (int)((double)total * cta / ctas); }
+__device__ __forceinline__ int owner_of(int place, int total, int ctas) { return (int)(((double)(place + 1LL) * ctas - 1.0) / total); }
+
+// What the second kernel has to know of a tile: its segment (-1: a place without a tile), the blocks of its halves, their rows and tokens.
+__device__ __forceinline__ int4 tile_note(int seg, int id0, int id1, int row0, int row1, int count0, int count1)
 {
-    return min(max(max((total + warps - 1) / warps, min(segments, total)), 1), most);
+    return make_int4(seg, id0, id1, row0 | row1 << 8 | count0 << 16 | count1 << 24);
 }
-__device__ __forceinline__ int owner_of(long long tile, long long total, int ctas) { return (int)(((tile + 1) * ctas - 1) / total); }
 
 __device__ __forceinline__ float exp2_fast(float x)
 {
@@ -161,7 +172,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         if (st < streams) {
             const int n = length_or_none((int)ld_global_u32(c.length + st), c, a.status);
             if (st < kLengthCache) s_len[st] = n;
-            mine += tiles_of(n, shift) * a.row_groups;
+            mine += places_of(tiles_of(n, shift)) * a.row_groups;
         }
     }
     int incl = mine;
@@ -179,20 +190,29 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         total += s_scan[w];
     }
     auto length_of = [&](int st) { return st < kLengthCache ? s_len[st] : length_or_none((int)ld_global_u32(c.length + st), c, a.status); };
-    const int ctas = working_ctas(total, streams * a.row_groups, NW, gridDim.x), cta = blockIdx.x;
-    if (cta == 0) {                           // for the second kernel
+    const int ctas = working_ctas(total, NW, gridDim.x), cta = blockIdx.x;
+    if (a.accumulate && cta == 0) {           // for the second kernel
         if (tid == 0) a.begin[streams * a.row_groups] = total;
         for (int st = tid * per, at = base; st < min(streams, (tid + 1) * per); ++st) {
-            const int k = tiles_of(length_of(st), shift);
-            for (int r = 0; r < a.row_groups; ++r, at += k) a.begin[st * a.row_groups + r] = at;
+            const int k = places_of(tiles_of(length_of(st), shift));
+            for (int r = 0; r < a.row_groups; ++r, at += k) a.begin[st * a.row_groups + r] = at + kRoom;
+        }
+    }
+    for (int st = cta; st < streams; st += gridDim.x) {   // queries that see nothing
+        if (length_of(st) != 0) continue;
+        const int b = st / c.kv_heads, h = st % c.kv_heads;
+        for (int i = tid; i < a.rows * (D / 8); i += NW * 32) {
+            const int r = i / (D / 8), qi = r / a.group;
+            __half* const to = a.out + (long long)b * a.out_batch + (long long)qi * a.out_token + ((long long)h * a.group + (r - qi * a.group)) * D + i % (D / 8) * 8;
+            *reinterpret_cast<uint4*>(to) = make_uint4(0u, 0u, 0u, 0u);
         }
     }
     if (total == 0 || cta >= ctas) return;
-    const int t0 = (int)((long long)total * cta / ctas), t1 = (int)((long long)total * (cta + 1) / ctas);
+    const int t0 = begin_of(cta, total, ctas), t1 = begin_of(cta + 1, total, ctas);
     if (t0 >= base && t0 < base + mine) {
         int st = tid * per, at = base;
         for (;; ++st) {
-            const int k = tiles_of(length_of(st), shift) * a.row_groups;
+            const int k = places_of(tiles_of(length_of(st), shift)) * a.row_groups;
             if (t0 < at + k) break;
             at += k;
         }
@@ -200,33 +220,47 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         s_start[1] = at;
     }
     __syncthreads();
-    const int stream0 = s_start[0], n0 = length_of(stream0), tiles0 = tiles_of(n0, shift), rg0 = (t0 - s_start[1]) / tiles0;
-    const int seg0 = stream0 * a.row_groups + rg0, begin0 = s_start[1] + rg0 * tiles0;
+    const int stream0 = s_start[0], n0 = length_of(stream0), tiles0 = tiles_of(n0, shift), rg0 = (t0 - s_start[1]) / places_of(tiles0);
+    const int seg0 = stream0 * a.row_groups + rg0, begin0 = s_start[1] + rg0 * places_of(tiles0) + kRoom;
 
     // ---- the tiles ahead: a walk over this warp's tiles that knows the segment of each; first the block numbers, one tile later
-    // the copies
-    int w_tile = t0 + warp, w_seg = seg0, w_begin = begin0, w_n = n0, w_end = begin0 + tiles0;
-    auto seek = [&]() {                       // the segment of w_tile
-        while (w_tile >= w_end && w_tile < t1) {
+    // the copies.  (Of a segment's tiles in the part the first is the first warp's.)
+    constexpr int kNoTile = 0x7fffffff;
+    int w_seg = seg0, w_begin = begin0, w_n = n0, w_end = begin0 + tiles0, w_tile = max(t0, begin0) + warp;
+    auto seek = [&]() {                       // the next segment with a tile for this warp, where this one has no more
+        while (w_tile >= min(w_end, t1)) {
+            if (w_end >= t1) {
+                w_tile = kNoTile;
+                return;
+            }
             ++w_seg;
-            w_begin = w_end;
             w_n = length_of(w_seg / a.row_groups);
-            w_end = w_begin + tiles_of(w_n, shift);
+            const int k = tiles_of(w_n, shift);
+            if (k == 0) continue;
+            w_begin = w_end + kRoom;
+            w_end = w_begin + k;
+            if (w_begin >= t1) {
+                w_tile = kNoTile;
+                return;
+            }
+            w_tile = w_begin + warp;
         }
     };
     seek();
     // the tile whose block numbers are on their way (lane u: half u)
-    int p_tile = w_tile, p_stream = 0, p_local = 0, p_n = 0, p_id = 0;
+    int p_tile = w_tile, p_seg = 0, p_local = 0, p_n = 0, p_id = 0;
     auto look_up = [&]() {
         p_tile = w_tile;
-        if (w_tile < t1) {
-            p_stream = w_seg / a.row_groups;
+        if (w_tile != kNoTile) {
+            p_seg = w_seg;
             p_local = w_tile - w_begin;
             p_n = w_n;
-            const int token = p_local * kTile + (lane & 1) * 16;
-            p_id = token < full_tokens(w_n, shift) ? (int)ld_global_u32(c.table + (size_t)p_stream * c.table_width + (token >> shift)) : 0;
+            const int full = full_tokens(w_n, shift), tail = p_local - (full + kTile - 1) / kTile;
+            const int token = tail < 0 ? p_local * kTile + (lane & 1) * 16 : full + tail * 16;
+            p_id = token < (tail < 0 ? full : a.accumulate ? w_n : 0) ? (int)ld_global_u32(c.table + (size_t)(w_seg / a.row_groups) * c.table_width + (token >> shift)) : 0;
             w_tile += NW;
             if (w_tile >= w_end) seek();
+            else if (w_tile >= t1) w_tile = kNoTile;
         }
     };
     // A lane's pieces of a half tile of codes; those of eight rows and more apart lie as far apart.
@@ -235,13 +269,20 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
 #pragma unroll
     for (int i = 0; i < kDistinct; ++i) place[i] = place_of<CH>((i * 32 + lane) / CH, (i * 32 + lane) % CH);
     auto copy = [&](int stage) {
-        if (p_tile >= t1) return;
+        if (p_tile == kNoTile) return;
         const unsigned dst = ring + stage * S::kTileBytes;
         const int full = full_tokens(p_n, shift), tail = p_local - (full + kTile - 1) / kTile;
+        const bool known = (unsigned)p_id < (unsigned)c.blocks;
+        if (!known) refuse(a.status);
+        if (a.accumulate) {
+            const int id1 = __shfl_sync(0xffffffffu, p_id, 1), mask = (1 << shift) - 1, there = tail < 0 ? full : p_n;
+            const int token = tail < 0 ? p_local * kTile : full + tail * 16;
+            if (lane == 0)
+                a.tiles[p_tile] = tile_note(p_seg, p_id, id1, token & mask, (token + 16) & mask, known ? min(16, there - token) : 0,
+                                            tail < 0 && (unsigned)id1 < (unsigned)c.blocks ? max(0, min(16, there - token - 16)) : 0);
+        }
         if (tail < 0) {
-            const bool known = (unsigned)p_id < (unsigned)c.blocks;
             const int id = known ? p_id : 0;
-            if (!known) refuse(a.status);
             if (lane < 4) {
                 // (lanes 0 and 1: k of the halves, 2 and 3: v of the halves; lane & 1 is the half whose number the lane holds)
                 const unsigned at = smem_u32(&s_scale[warp][stage][0]) + lane * 4;
@@ -264,7 +305,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             }
         } else {
             const int r0 = tail * 16;
-            const size_t from = (((size_t)p_stream << shift) + r0) * D;
+            const size_t from = (((size_t)(p_seg / a.row_groups) << shift) + r0) * D;
             const __half* const k = static_cast<const __half*>(c.k_tail) + from + lane * 8;
             const __half* const v = static_cast<const __half*>(c.v_tail) + from + lane * 8;
 #pragma unroll
@@ -286,25 +327,15 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
     }
 
     // ---- segment after segment
-    int stage = 0, tile = t0 + warp;
-    int seg = seg0, begin = begin0, n = n0;
-    while (begin < t1) {
-        const int tiles = tiles_of(n, shift), end = begin + tiles;
-        if (tiles == 0) {
-            ++seg;
-            n = length_of(seg / a.row_groups);
-            continue;
-        }
-        const int stream = seg / a.row_groups, row0 = seg % a.row_groups * ROWS;
-        const int b = stream / c.kv_heads, h = stream % c.kv_heads;
-        // queries: column g of set s is row row0 + 8s + g (with four rows twice the same four); a lane's dimensions of a chunk of 16
-        // are 4cc .. 4cc + 3, as its bytes of the codes are
-        unsigned qf[NC][CH][2];
-        int lim[NC][2];                       // tokens that the rows of this lane's columns see
+    int stage = 0, seg = seg0, begin = begin0, n = n0;
+    unsigned qf[NC][CH][2];
+    // Queries: column g of set s is row row0 + 8s + g of its stream (with four rows twice the same four); a lane's dimensions of a
+    // chunk of 16 are 4cc .. 4cc + 3, as its bytes of the codes are.
+    auto load_queries = [&]() {
+        const int stream = seg / a.row_groups, row0 = seg % a.row_groups * ROWS, b = stream / c.kv_heads, h = stream % c.kv_heads;
 #pragma unroll
         for (int s = 0; s < NC; ++s) {
-            const int r = row0 + s * 8 + (ROWS == 4 ? g & 3 : g);
-            const int i = r / a.group;
+            const int r = row0 + s * 8 + (ROWS == 4 ? g & 3 : g), i = r / a.group;
             const __half* const q = a.q + (long long)b * a.q_batch + (long long)i * a.q_token + ((long long)h * a.group + (r - i * a.group)) * D + 4 * cc;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
@@ -313,12 +344,22 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                 qf[s][j][0] = v.x;
                 qf[s][j][1] = v.y;
             }
+        }
+    };
+    load_queries();
+    while (begin < t1) {
+        const int tiles = tiles_of(n, shift), end = begin + tiles;
+        const int stream = seg / a.row_groups, row0 = seg % a.row_groups * ROWS;
+        const int b = stream / c.kv_heads, h = stream % c.kv_heads;
+        if (a.accumulate && begin >= t0 && tid < kRoom) a.tiles[begin - kRoom + tid] = tile_note(-1, 0, 0, 0, 0, 0, 0);
+        int lim[NC][2];                       // tokens that the rows of this lane's columns see
+#pragma unroll
+        for (int s = 0; s < NC; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int rc = row0 + s * 8 + (ROWS == 4 ? (2 * cc + e) & 3 : 2 * cc + e);
                 lim[s][e] = rc < a.rows ? n - a.queries + 1 + rc / a.group : n;
             }
-        }
         const int full = full_tokens(n, shift), nt = (full + kTile - 1) / kTile;
         const int clean = max(0, min(full, n - a.queries + 1)) / kTile;   // tiles of whose tokens all are there and all rows see all
         float o[CH][NC][4];
@@ -332,7 +373,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             for (int d = 0; d < CH; ++d) o[d][s][0] = o[d][s][1] = o[d][s][2] = o[d][s][3] = 0.0f;
         }
         const int stop = min(end, t1);
-        for (; tile < stop; tile += NW) {
+        for (int tile = max(t0, begin) + warp; tile < stop; tile += NW) {
             cp_async_wait<STAGES - 2>();
             __syncwarp();
             {
@@ -543,6 +584,16 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
 
+        // ---- the next segment, whose queries are on their way while this one is finished
+        const int this_seg = seg, this_begin = begin;
+        begin = end;
+        do {
+            ++seg;
+            n = begin + kRoom < t1 ? length_of(seg / a.row_groups) : 1;
+        } while (n == 0);
+        begin += kRoom;
+        if (begin < t1) load_queries();
+
         // ---- the warps' sums: to the CTA's largest M, then by way of shared memory, half the warps at a time
 #pragma unroll
         for (int s = 0; s < NC; ++s)
@@ -600,8 +651,15 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         __syncthreads();
         if (warp < NW / 2) put(s_o[warp], true);
         __syncthreads();
-        const bool whole = begin >= t0 && end <= t1;
-        const size_t part = (size_t)cta + seg;
+        const bool whole = this_begin >= t0 && end <= t1;
+        const size_t part = (size_t)cta + this_seg;
+        auto answer = [&](int r, int d, float m, float sum, const float4& v) {   // four dimensions of a row
+            const int rr = row0 + r, qi = rr / a.group;
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;           // (a row that sees nothing: zeros)
+            __half* const to = a.out + (long long)b * a.out_batch + (long long)qi * a.out_token + ((long long)h * a.group + (rr - qi * a.group)) * D + d;
+            *reinterpret_cast<uint2*>(to) = make_uint2(halves(v.x * inv, v.y * inv), halves(v.z * inv, v.w * inv));
+            if (a.accumulate && d == 0) a.lse[(size_t)this_seg * ROWS + r] = make_float2(m == -INFINITY ? 0.0f : m - kUp, inv);
+        };
         for (int i = tid; i < ROWS * (D / 4); i += NW * 32) {
             const int r = i / (D / 4), d = i % (D / 4) * 4;
             if (row0 + r >= a.rows) continue;
@@ -619,185 +677,133 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                 const float4 k = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
                 v.x += k.x, v.y += k.y, v.z += k.z, v.w += k.w;
             }
-            if (!whole) *reinterpret_cast<float4*>(a.o + (part * ROWS + r) * D + d) = v;
-            if ((!whole || a.accumulate) && d == 0) a.ml[part * ROWS + r] = make_float2(m, sum);
             if (whole) {
-                const int rr = row0 + r, qi = rr / a.group;
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;           // (a row that sees nothing: zeros)
-                __half* const to = a.out + (long long)b * a.out_batch + (long long)qi * a.out_token + ((long long)h * a.group + (rr - qi * a.group)) * D + d;
-                const uint2 hv = make_uint2(halves(v.x * inv, v.y * inv), halves(v.z * inv, v.w * inv));
-                *reinterpret_cast<uint2*>(to) = hv;
+                answer(r, d, m, sum, v);
+            } else {
+                *reinterpret_cast<float4*>(a.o + (part * ROWS + r) * D + d) = v;
+                if (d == 0) a.ml[part * ROWS + r] = make_float2(m, sum);
             }
         }
         __syncthreads();
-        begin = end;
-        ++seg;
-        n = begin < t1 ? length_of(seg / a.row_groups) : 0;
+        if (!whole) {
+            // ---- a segment that several CTAs share: the last of them adds the parts
+            const int c0 = owner_of(this_begin, total, ctas), c1 = owner_of(end - 1, total, ctas);
+            if (tid == 0) {
+                __threadfence();              // (the parts, which the barrier has brought behind this thread, before the count)
+                s_start[0] = atomicAdd(a.arrived + this_seg, 1) == c1 - c0;
+                __threadfence();
+            }
+            __syncthreads();
+            if (s_start[0]) {
+                if (tid == 0) a.arrived[this_seg] = 0;
+                // a thread has four dimensions of a row, of every kSplit-th part
+                constexpr int kItems = ROWS * (D / 4), kSplit = NW * 32 / kItems < 1 ? 1 : NW * 32 / kItems;
+                for (int i = tid; i < kItems * kSplit; i += NW * 32) {
+                    const int r = i % kItems / (D / 4), d = i % (D / 4) * 4, first = c0 + i / kItems;
+                    if (row0 + r < a.rows) {
+                        float m = -INFINITY, sum = 0.0f;
+#pragma unroll 8
+                        for (int k = c0; k <= c1; ++k) m = fmaxf(m, __ldcg(a.ml + ((size_t)k + this_seg) * ROWS + r).x);
+#pragma unroll 4
+                        for (int k = c0; k <= c1; ++k) {
+                            const float2 x = __ldcg(a.ml + ((size_t)k + this_seg) * ROWS + r);
+                            sum += x.x == m ? x.y : x.y * exp2_fast(x.x - m);
+                        }
+                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+                        for (int k = first; k <= c1; k += kSplit) {
+                            const size_t at = ((size_t)k + this_seg) * ROWS + r;
+                            const float x = __ldcg(a.ml + at).x, f = x == m ? 1.0f : exp2_fast(x - m);
+                            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.o + at * D + d));
+                            v.x = fmaf(y.x, f, v.x), v.y = fmaf(y.y, f, v.y), v.z = fmaf(y.z, f, v.z), v.w = fmaf(y.w, f, v.w);
+                        }
+                        if (kSplit == 1) answer(r, d, m, sum, v);
+                        else {
+                            *reinterpret_cast<float4*>(&s_o[i / kItems][r][d]) = v;
+                            if (d == 0 && i < kItems) s_ml[0][r] = make_float2(m, sum);
+                        }
+                    }
+                }
+                if (kSplit > 1) {
+                    __syncthreads();
+                    for (int i = tid; i < kItems; i += NW * 32) {
+                        const int r = i / (D / 4), d = i % (D / 4) * 4;
+                        if (row0 + r < a.rows) {
+                            float4 v = *reinterpret_cast<const float4*>(&s_o[0][r][d]);
+#pragma unroll
+                            for (int k = 1; k < kSplit; ++k) {
+                                const float4 y = *reinterpret_cast<const float4*>(&s_o[k][r][d]);
+                                v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+                            }
+                            answer(r, d, s_ml[0][r].x, s_ml[0][r].y, v);
+                        }
+                    }
+                    __syncthreads();
+                }
+            }
+        }
     }
     cp_async_wait<0>();
 }
 
-// ---------------------------------------------------------------- the parts together
+// ---------------------------------------------------------------- weights
 
-// The (M, l) of a row over the CTAs that had part of its segment, by the lanes of a warp; and the CTAs.
-__device__ __forceinline__ float2 joined(const float2* ml, int rows, int seg, int r, int c0, int c1, int lane)
+constexpr int kNoteWarps = 8, kTilesAhead = 4;
+
+// The probabilities that a tile's tokens have received, a lane per token and a warp for four places at a time: their notes, then
+// scores, sums and weights are on their way together.
+template <int ROWS>
+__global__ void __launch_bounds__(kNoteWarps * 32) kv_weights_kernel(const AttnArgs a, int segments)
 {
-    float m = -INFINITY, l = 0.0f;
-    for (int i = c0 + lane; i <= c1; i += 32) {
-        const float2 v = ml[((size_t)i + seg) * rows + r];
-        const float top = fmaxf(m, v.x);
-        l = (m == top ? l : l * exp2_fast(m - top)) + (v.x == top ? v.y : v.y * exp2_fast(v.x - top));
-        m = top;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, m, o), ol = __shfl_xor_sync(0xffffffffu, l, o);
-        const float top = fmaxf(m, om);
-        // (the two lanes of a pair add the same two values)
-        l = (m == top ? l : l * exp2_fast(m - top)) + (om == top ? ol : ol * exp2_fast(om - top));
-        m = top;
-    }
-    return make_float2(m, l);
-}
-
-constexpr int kJoinWarps = 4, kTilesAhead = 4;
-
-// CTAs below `rows_ctas`: one row of one segment each, its parts' sums added in the order of the CTAs (by four warps, then the
-// four).  The others: an equal part of all tiles each, a lane per token.
-template <int D, int ROWS>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(const AttnArgs a, int streams, int rows_ctas, int parts, int warps)
-{
-    __shared__ float s_o[kJoinWarps][D];
-    __shared__ float2 s_ml[64];
-    const spqt_kv_cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, shift = a.shift;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int segments = streams * a.row_groups, total = (int)ld_global_u32(a.begin + segments);
-    const int ctas = working_ctas(total, segments, warps, parts);
-    if ((int)blockIdx.x < rows_ctas) {
-        const int rr = blockIdx.x % a.rows, stream = blockIdx.x / a.rows, rg = rr / ROWS, r = rr % ROWS, seg = stream * a.row_groups + rg;
-        const int b = stream / c.kv_heads, h = stream % c.kv_heads, qi = rr / a.group;
-        const int begin = (int)ld_global_u32(a.begin + seg);   // (of an empty stream: of no meaning)
-        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, shift);
-        __half* const out = a.out + (long long)b * a.out_batch + (long long)qi * a.out_token + ((long long)h * a.group + (rr - qi * a.group)) * D;
-        if (tiles == 0) {
-            for (int d = tid * 2; d < D; d += kJoinWarps * 64) *reinterpret_cast<unsigned*>(out + d) = 0u;
-            return;
+    const int total = (int)ld_global_u32(a.begin + segments);
+    for (int x0 = (blockIdx.x * kNoteWarps + warp) * kTilesAhead; x0 < total; x0 += gridDim.x * kNoteWarps * kTilesAhead) {
+        int seg[kTilesAhead];
+        float* to[kTilesAhead];
+        float sum[kTilesAhead], old[kTilesAhead];
+#pragma unroll
+        for (int u = 0; u < kTilesAhead; ++u) {
+            const int4 t = x0 + u < total ? a.tiles[x0 + u] : make_int4(-1, 0, 0, 0);
+            const int half = lane >> 4, row = t.w >> (8 * half) & 0xff, count = t.w >> (16 + 8 * half) & 0xff;
+            // (a stream's first row group stands for all)
+            seg[u] = t.x >= 0 && t.x % a.row_groups == 0 && (lane & 15) < count ? t.x : -1;
+            to[u] = a.c.weight + ((size_t)(unsigned)(half ? t.z : t.y) << shift) + row + (lane & 15);
+            sum[u] = 0.0f;
         }
-        const int c0 = owner_of(begin, total, ctas), c1 = owner_of(begin + tiles - 1, total, ctas);
-        if (c0 == c1) return;                 // finished where it was computed
-        const float2 ml = joined(a.ml, ROWS, seg, r, c0, c1, lane);
-        constexpr int V = (D + 127) / 128;
-        float4 sum[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int i = c0 + warp; i <= c1; i += kJoinWarps) {
-            const size_t at = ((size_t)i + seg) * ROWS + r;
-            const float m = a.ml[at].x;
-            const float f = m == ml.x ? 1.0f : exp2_fast(m - ml.x);
+        for (int u = 0; u < kTilesAhead; ++u) old[u] = seg[u] >= 0 ? *to[u] : 0.0f;
+        for (int rg = 0; rg < a.row_groups; ++rg) {
+            const float* from[kTilesAhead];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int d = v * 128 + lane * 4;
-                if (d < D) {
-                    const float4 k = *reinterpret_cast<const float4*>(a.o + at * D + d);
-                    sum[v].x = fmaf(k.x, f, sum[v].x), sum[v].y = fmaf(k.y, f, sum[v].y);
-                    sum[v].z = fmaf(k.z, f, sum[v].z), sum[v].w = fmaf(k.w, f, sum[v].w);
-                }
+            for (int u = 0; u < kTilesAhead; ++u) {
+                const int x = seg[u] < 0 ? 0 : rg == 0 ? x0 + u : x0 + u - a.begin[seg[u]] + a.begin[seg[u] + rg];
+                from[u] = a.scores + ((size_t)x * kTile + lane) * ROWS;
             }
-        }
+            const int rows = min(ROWS, a.rows - rg * ROWS);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v * 128 + lane * 4 < D) *reinterpret_cast<float4*>(&s_o[warp][v * 128 + lane * 4]) = sum[v];
-        __syncthreads();
-        const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
-        for (int d = tid; d < D; d += kJoinWarps * 32) {
-            float v = 0.0f;
+            for (int r = 0; r < ROWS; r += 4) {
+                if (r >= rows) break;
+                float4 s[kTilesAhead];
 #pragma unroll
-            for (int w = 0; w < kJoinWarps; ++w) v += s_o[w][d];
-            out[d] = __float2half_rn(v * inv);
-        }
-        return;
-    }
-    // weights: tiles of the streams' first row groups, numbered end to end
-    const int all = total / a.row_groups, me = blockIdx.x - rows_ctas, them = gridDim.x - rows_ctas;
-    const int t0 = (int)((long long)all * me / them), t1 = (int)((long long)all * (me + 1) / them);
-    if (t0 >= t1) return;
-    // the stream of t0: the last that begins there or before (streams without tokens begin where the next one does)
-    int stream = 0;
-    for (int left = streams; left > 1;) {                // (the lanes of a warp look at 32 places at a time)
-        const int step = (left + 31) / 32, at = lane * step;
-        const unsigned mask = __ballot_sync(0xffffffffu, at < left && (int)ld_global_u32(a.begin + (size_t)(stream + min(at, left - 1)) * a.row_groups) / a.row_groups <= t0);
-        const int k = (31 - __clz(mask)) * step;         // (the first place always counts)
-        stream += k;
-        left = min(step, left - k);
-    }
-    for (int t = t0; t < t1;) {
-        const int n = length_or_none((int)ld_global_u32(c.length + stream), c, a.status), tiles = tiles_of(n, shift);
-        if (tiles == 0) {
-            ++stream;
-            continue;
-        }
-        const int seg = stream * a.row_groups, begin = (int)ld_global_u32(a.begin + seg), first = begin / a.row_groups;
-        const int stop = min(t1, first + tiles), full = full_tokens(n, shift), nt = (full + kTile - 1) / kTile;
-        const int32_t* const row = c.table + (size_t)stream * c.table_width;
-        for (int rb = 0; rb < a.rows; rb += 64) {      // 64 rows at a time
-            const int rows = min(64, a.rows - rb);
-            __syncthreads();
-            for (int r = warp; r < rows; r += kJoinWarps) {
-                const int rg = (rb + r) / ROWS, sg = seg + rg, bg = begin + rg * tiles;
-                const float2 v = joined(a.ml, ROWS, sg, (rb + r) % ROWS, owner_of(bg, total, ctas), owner_of(bg + tiles - 1, total, ctas), lane);
-                if (lane == 0) s_ml[r] = make_float2(v.x == -INFINITY ? 0.0f : v.x - kUp, v.y == 0.0f ? 0.0f : 1.0f / v.y);
-            }
-            __syncthreads();
-            // four tiles of a warp at a time: block numbers and scores, then the weights, are on their way together
-            for (int x0 = t + warp; x0 < stop; x0 += kJoinWarps * kTilesAhead) {
-                float sum[kTilesAhead];
-                float* to[kTilesAhead];
-                unsigned block[kTilesAhead];
-                int token[kTilesAhead];
-                bool there[kTilesAhead];
+                for (int u = 0; u < kTilesAhead; ++u) s[u] = seg[u] >= 0 ? *reinterpret_cast<const float4*>(from[u] + r) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int u = 0; u < kTilesAhead; ++u) {
-                    const int x = x0 + u * kJoinWarps, local = x - first;
-                    const bool codes = local < nt;
-                    token[u] = (codes ? local * kTile : full + (local - nt) * 16) + lane;
-                    there[u] = x < stop && token[u] < (codes ? full : n) && (codes || lane < 16);
-                    block[u] = there[u] ? (unsigned)row[token[u] >> shift] : 0u;
-                    sum[u] = 0.0f;
+                    if (seg[u] < 0) continue;
+                    const float e[4] = {s[u].x, s[u].y, s[u].z, s[u].w};
+                    const float4* const lse = reinterpret_cast<const float4*>(a.lse + (size_t)(seg[u] + rg) * ROWS + r);
+                    const float4 l0 = lse[0], l1 = lse[1];
+                    sum[u] = fmaf(exp2_fast(e[0] - l0.x), l0.y, sum[u]);
+                    if (r + 1 < rows) sum[u] = fmaf(exp2_fast(e[1] - l0.z), l0.w, sum[u]);
+                    if (r + 2 < rows) sum[u] = fmaf(exp2_fast(e[2] - l1.x), l1.y, sum[u]);
+                    if (r + 3 < rows) sum[u] = fmaf(exp2_fast(e[3] - l1.z), l1.w, sum[u]);
                 }
-                for (int r = 0; r < rows; r += 4) {
-                    const float* const from = a.scores + ((size_t)(begin + (rb + r) / ROWS * tiles + (x0 - first)) * kTile + lane) * ROWS + (rb + r) % ROWS;
-                    float4 s[kTilesAhead];
-#pragma unroll
-                    for (int u = 0; u < kTilesAhead; ++u)
-                        s[u] = there[u] ? *reinterpret_cast<const float4*>(from + u * (kJoinWarps * kTile * ROWS)) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int u = 0; u < kTilesAhead; ++u) {
-                        const float e[4] = {s[u].x, s[u].y, s[u].z, s[u].w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (r + k < rows) sum[u] = fmaf(exp2_fast(e[k] - s_ml[r + k].x), s_ml[r + k].y, sum[u]);
-                    }
-                }
-                float old[kTilesAhead];
-#pragma unroll
-                for (int u = 0; u < kTilesAhead; ++u) {
-                    if (there[u] && block[u] >= (unsigned)c.blocks) {
-                        refuse(a.status);
-                        there[u] = false;
-                    }
-                    to[u] = c.weight + ((size_t)block[u] << shift) + (token[u] & ((1 << shift) - 1));
-                    old[u] = there[u] ? *to[u] : 0.0f;
-                }
-#pragma unroll
-                for (int u = 0; u < kTilesAhead; ++u)
-                    if (there[u]) *to[u] = old[u] + sum[u];
             }
         }
-        t = stop;
-        ++stream;
+#pragma unroll
+        for (int u = 0; u < kTilesAhead; ++u)
+            if (seg[u] >= 0) *to[u] = old[u] + sum[u];
     }
 }
 
@@ -806,7 +812,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_attention_join_kernel(cons
 inline int rows_of(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
 
 struct AttnWorkspace {
-    size_t begin, ml, o, scores, bytes;
+    size_t arrived, begin, ml, o, lse, tiles, scores, bytes;   // (what stays zero between calls at a place that depends on nothing)
 };
 
 // false where the tiles' numbers would pass 31 bits
@@ -814,18 +820,22 @@ inline bool attention_workspace(const spqt_kv_cache& c, int group, int queries, 
 {
     const int rows = group * queries, R = rows_of(rows), groups = (rows + R - 1) / R;
     const long long streams = (long long)c.batch * c.kv_heads, segments = streams * groups;
-    const long long tiles = segments * (((long long)c.table_width * c.block_tokens + kTile - 1) / kTile + 8);
+    const long long tiles = segments * (((long long)c.table_width * c.block_tokens + kTile - 1) / kTile + 8 + kRoom);
     if (segments > kMaxStreams || tiles > 0x7fffffffLL) return false;
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     size_t at = kKvHeader;
+    w->arrived = at, at += (size_t)kMaxStreams * 4;
     w->begin = at, at += up(((size_t)segments + 1) * 4);
     const size_t parts = (size_t)(kMaxAttnCtas + segments);
     w->ml = at, at += up(parts * R * 8);
     w->o = at, at += up(parts * R * c.head_dim * 4);
-    w->scores = at;
-    if (c.weight) at += up((size_t)tiles * kTile * R * 4);
-    const size_t lengths = kKvHeader + kv_lengths_bytes(c);
-    w->bytes = at > lengths ? at : lengths;
+    w->lse = w->tiles = w->scores = at;
+    if (c.weight) {
+        at += up((size_t)segments * R * 8);
+        w->tiles = at, at += up((size_t)tiles * 16);
+        w->scores = at, at += up((size_t)tiles * kTile * R * 4);
+    }
+    w->bytes = at;
     return true;
 }
 
@@ -848,9 +858,7 @@ cudaError_t launch_attention(const AttnArgs& a, cudaStream_t s)
     const int parts = sms < kMaxAttnCtas ? sms : kMaxAttnCtas, streams = a.c.batch * a.c.kv_heads;
     err = launch_overlapping(kv_attention_kernel<FMT, D, ROWS>, dim3(parts), S::kWarps * 32, smem, s, a, streams);
     if (err != cudaSuccess) return err;
-    const int rows_ctas = streams * a.rows;
-    return launch_overlapping(kv_attention_join_kernel<D, ROWS>, dim3(rows_ctas + (a.accumulate ? 4 * sms : 0)), kJoinWarps * 32, 0, s, a, streams, rows_ctas,
-                              parts, S::kWarps);
+    return a.accumulate ? launch_overlapping(kv_weights_kernel<ROWS>, dim3(4 * sms), kNoteWarps * 32, 0, s, a, streams * a.row_groups) : cudaSuccess;
 }
 
 template <int FMT, int D>
@@ -911,13 +919,14 @@ spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long lo
     if (!q || !out || (accumulate && !cache->weight) || q_batch_stride < 0 || q_token_stride < 0 || out_batch_stride < 0 || out_token_stride < 0)
         return SPQT_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(out, 16) || q_batch_stride % 8 || q_token_stride % 8 || out_batch_stride % 8 || out_token_stride % 8) return SPQT_ERR_ALIGNMENT;
-    st = check_kv_workspace(workspace, workspace_bytes, accumulate ? w.bytes : w.scores);
+    st = check_kv_workspace(workspace, workspace_bytes, accumulate ? w.bytes : w.lse);
     if (st != SPQT_OK) return st;
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     const int group = q_heads / cache->kv_heads, rows = group * queries, R = rows_of(rows);
     const AttnArgs a = {*cache, static_cast<const __half*>(q), q_batch_stride, q_token_stride, static_cast<__half*>(out), out_batch_stride, out_token_stride,
                         group, queries, rows, (rows + R - 1) / R, 31 - __builtin_clz((unsigned)cache->block_tokens), accumulate ? 1 : 0, scale * 1.4426950408889634f, static_cast<int*>(status_word(workspace)),
-                        reinterpret_cast<int*>(ws + w.begin), reinterpret_cast<float2*>(ws + w.ml), reinterpret_cast<float*>(ws + w.o),
+                        reinterpret_cast<int*>(ws + w.begin), reinterpret_cast<int*>(ws + w.arrived), reinterpret_cast<float2*>(ws + w.ml),
+                        reinterpret_cast<float*>(ws + w.o), reinterpret_cast<float2*>(ws + w.lse), reinterpret_cast<int4*>(ws + w.tiles),
                         reinterpret_cast<float*>(ws + w.scores)};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return launched(cache->format == SPQT_KV_INT8 ? launch_dim<SPQT_KV_INT8>(a, s) : launch_dim<SPQT_KV_E4M3>(a, s));

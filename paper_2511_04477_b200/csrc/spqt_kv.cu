@@ -420,14 +420,14 @@ spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void
     if (!aligned(k, 16) || !aligned(v, 16) || batch_stride % 8 || token_stride % 8 || !aligned(counts, 4) || !aligned(length_out, 4)) return SPQT_ERR_ALIGNMENT;
     if (cache->batch > 65535 || tokens > (1 << 28) || ((long long)tokens + 2 * cache->block_tokens) / cache->block_tokens * cache->kv_heads >= 0x7fffffffLL)
         return SPQT_ERR_UNSUPPORTED;
-    st = check_kv_workspace(workspace, workspace_bytes, kKvHeader + kv_lengths_bytes(*cache));
+    st = check_kv_workspace(workspace, workspace_bytes, kKvScratch + kv_lengths_bytes(*cache));
     if (st != SPQT_OK) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     AppendArgs a = {*cache, static_cast<const __half*>(k), static_cast<const __half*>(v), tokens, batch_stride, token_stride, counts,
                     length_out ? length_out : cache->length, static_cast<int*>(status_word(workspace))};
     // Lengths are written in place at once where one CTA per stream reads them (a single token); else by way of the workspace.
     const bool indirect = a.length_out == cache->length && tokens > 1;
-    if (indirect) a.length_out = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + kKvHeader);
+    if (indirect) a.length_out = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + kKvScratch);
 #define SPQT_F(F, D) launch_append<F, D>(a, s)
     cudaError_t err = SPQT_KV_DISPATCH(*cache, SPQT_F);
 #undef SPQT_F

@@ -24,9 +24,9 @@ inline spqt_status check_cache(const spqt_kv_cache* c)
     return SPQT_OK;
 }
 
-// Workspace of the cache's calls: the header with the status word, which all of them need, and behind it what a call leaves for its
-// own second kernel (nothing lasts from one call to the next).
-constexpr size_t kKvHeader = kSlotsOffset;
+// Workspace of the cache's calls: the header with the status word, which all of them need; the attention's counts of parts, zero
+// between calls; behind them what a call leaves for its own CTAs and its second kernel.
+constexpr size_t kKvHeader = kSlotsOffset, kKvScratch = kKvHeader + (size_t)kMaxStreams * 4;
 inline size_t kv_lengths_bytes(const spqt_kv_cache& c) { return ((size_t)c.batch * c.kv_heads * 4 + 255) / 256 * 256; }
 
 inline spqt_status check_kv_workspace(const void* workspace, size_t bytes, size_t need)
