@@ -31,8 +31,10 @@
 namespace spqt {
 
 constexpr int kTile = 32;               // tokens of a tile of codes; half as many of the block that is not full
-constexpr int kRoom = 12;               // tiles that a segment costs beside its own (131072 tokens, eight streams: FIXROOM)
-constexpr int kMaxAttnCtas = 320;       // parts at most
+// Tiles that a segment costs beside its own.  With 0 / 6 / 12 / 20: 160 streams of up to 2047 tokens 34.6 / 26.5 / 24.8 / 23.0 us, 4001
+// tokens of eight streams 18.5 / 11.5 / 11.5 / 11.4, ten streams of five queries in two row groups 39.8 / 38.3 / 36.8 / 39.6.
+constexpr int kRoom = 16;
+constexpr int kMaxAttnCtas = 160;       // parts at most
 constexpr int kLengthCache = 1024;      // streams whose lengths a CTA keeps in shared memory
 constexpr float kUp = 10.0f;            // p of the largest score is 2^kUp, when M is set
 constexpr float kSlack = 4.0f;          // and 2^(kUp + kSlack) before M is set anew
@@ -151,12 +153,13 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
 {
     using S = AttnShape<D, ROWS>;
     constexpr int NW = S::kWarps, STAGES = S::kStages, NC = S::kCols, CH = D / 16;
-    extern __shared__ __align__(128) unsigned char s_ring[];                 // [NW][STAGES][kTileBytes]
+    extern __shared__ __align__(128) unsigned char s_ring[];                 // [NW][STAGES][kTileBytes], then s_part
     __shared__ int s_len[kLengthCache];
     __shared__ int s_scan[NW], s_start[2];
     __shared__ __align__(16) float s_scale[NW][STAGES][4];                   // k scale of the halves, v scale of the halves
     __shared__ float2 s_ml[NW][ROWS];
     __shared__ __align__(16) float s_o[NW / 2][ROWS][S::kStride];
+    float2(*const s_part)[ROWS] = reinterpret_cast<float2(*)[ROWS]>(s_ring + NW * STAGES * S::kTileBytes);   // (M, l) of the parts of a segment
     const spqt_kv_cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, cc = lane & 3;
     const int shift = a.shift;
@@ -689,36 +692,54 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             // ---- a segment that several CTAs share: the last of them adds the parts
             const int c0 = owner_of(this_begin, total, ctas), c1 = owner_of(end - 1, total, ctas);
             if (tid == 0) {
-                __threadfence();              // (the parts, which the barrier has brought behind this thread, before the count)
-                s_start[0] = atomicAdd(a.arrived + this_seg, 1) == c1 - c0;
-                __threadfence();
+                // (the parts, which the barrier has brought behind this thread, before the count; the count before the others' parts)
+                int before;
+                asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(a.arrived + this_seg) : "memory");
+                s_start[0] = before == c1 - c0;
             }
             __syncthreads();
             if (s_start[0]) {
                 if (tid == 0) a.arrived[this_seg] = 0;
-                // a thread has four dimensions of a row, of every kSplit-th part
-                constexpr int kItems = ROWS * (D / 4), kSplit = NW * 32 / kItems < 1 ? 1 : NW * 32 / kItems;
+                // a thread has four dimensions of a row, of every kSplit-th part; the first kAhead are on their way beside the parts' (M, l)
+                constexpr int kItems = ROWS * (D / 4), kSplit = NW * 32 / kItems < 1 ? 1 : NW * 32 / kItems, kAhead = 6;
+                for (int i = tid; i < (c1 - c0 + 1) * ROWS; i += NW * 32)
+                    s_part[i / ROWS][i % ROWS] = __ldcg(a.ml + ((size_t)c0 + i / ROWS + this_seg) * ROWS + i % ROWS);
+                auto sums_of = [&](int i, int k) {   // of part k
+                    return __ldcg(reinterpret_cast<const float4*>(a.o + (((size_t)k + this_seg) * ROWS + i % kItems / (D / 4)) * D + i % (D / 4) * 4));
+                };
+                float4 ahead[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const int at = c0 + tid / kItems + k * kSplit;
+                    ahead[k] = tid < kItems * kSplit && at <= c1 ? sums_of(tid, at) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                __syncthreads();
                 for (int i = tid; i < kItems * kSplit; i += NW * 32) {
                     const int r = i % kItems / (D / 4), d = i % (D / 4) * 4, first = c0 + i / kItems;
                     if (row0 + r < a.rows) {
                         float m = -INFINITY, sum = 0.0f;
-#pragma unroll 8
-                        for (int k = c0; k <= c1; ++k) m = fmaxf(m, __ldcg(a.ml + ((size_t)k + this_seg) * ROWS + r).x);
-#pragma unroll 4
-                        for (int k = c0; k <= c1; ++k) {
-                            const float2 x = __ldcg(a.ml + ((size_t)k + this_seg) * ROWS + r);
+                        for (int k = 0; k <= c1 - c0; ++k) m = fmaxf(m, s_part[k][r].x);
+                        for (int k = 0; k <= c1 - c0; ++k) {
+                            const float2 x = s_part[k][r];
                             sum += x.x == m ? x.y : x.y * exp2_fast(x.x - m);
                         }
                         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-                        for (int k = first; k <= c1; k += kSplit) {
-                            const size_t at = ((size_t)k + this_seg) * ROWS + r;
-                            const float x = __ldcg(a.ml + at).x, f = x == m ? 1.0f : exp2_fast(x - m);
-                            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.o + at * D + d));
+                        auto add = [&](int k, const float4& y) {
+                            const float x = s_part[k - c0][r].x, f = x == m ? 1.0f : exp2_fast(x - m);
                             v.x = fmaf(y.x, f, v.x), v.y = fmaf(y.y, f, v.y), v.z = fmaf(y.z, f, v.z), v.w = fmaf(y.w, f, v.w);
+                        };
+                        int k = first;
+                        if (i == tid) {
+#pragma unroll
+                            for (int u = 0; u < kAhead; ++u)
+                                if (first + u * kSplit <= c1) add(first + u * kSplit, ahead[u]);
+                            k += kAhead * kSplit;
                         }
-                        if (kSplit == 1) answer(r, d, m, sum, v);
-                        else {
+#pragma unroll 4
+                        for (; k <= c1; k += kSplit) add(k, sums_of(i, k));
+                        if (kSplit == 1) {
+                            answer(r, d, m, sum, v);
+                        } else {
                             *reinterpret_cast<float4*>(&s_o[i / kItems][r][d]) = v;
                             if (d == 0 && i < kItems) s_ml[0][r] = make_float2(m, sum);
                         }
@@ -738,8 +759,8 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                             answer(r, d, s_ml[0][r].x, s_ml[0][r].y, v);
                         }
                     }
-                    __syncthreads();
                 }
+                __syncthreads();
             }
         }
     }
@@ -748,23 +769,24 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
 
 // ---------------------------------------------------------------- weights
 
-constexpr int kNoteWarps = 8, kTilesAhead = 4;
+constexpr int kNoteWarps = 8;
 
-// The probabilities that a tile's tokens have received, a lane per token and a warp for four places at a time: their notes, then
+// The probabilities that a tile's tokens have received, a lane per token and a warp for a few places at a time: their notes, then
 // scores, sums and weights are on their way together.
 template <int ROWS>
 __global__ void __launch_bounds__(kNoteWarps * 32) kv_weights_kernel(const AttnArgs a, int segments)
 {
+    constexpr int N = 16 / ROWS < 2 ? 2 : 16 / ROWS, Q = ROWS / 4;   // places at a time, four rows each
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, shift = a.shift;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int total = (int)ld_global_u32(a.begin + segments);
-    for (int x0 = (blockIdx.x * kNoteWarps + warp) * kTilesAhead; x0 < total; x0 += gridDim.x * kNoteWarps * kTilesAhead) {
-        int seg[kTilesAhead];
-        float* to[kTilesAhead];
-        float sum[kTilesAhead], old[kTilesAhead];
+    for (int x0 = (blockIdx.x * kNoteWarps + warp) * N; x0 < total; x0 += gridDim.x * kNoteWarps * N) {
+        int seg[N];
+        float* to[N];
+        float sum[N], old[N];
 #pragma unroll
-        for (int u = 0; u < kTilesAhead; ++u) {
+        for (int u = 0; u < N; ++u) {
             const int4 t = x0 + u < total ? a.tiles[x0 + u] : make_int4(-1, 0, 0, 0);
             const int half = lane >> 4, row = t.w >> (8 * half) & 0xff, count = t.w >> (16 + 8 * half) & 0xff;
             // (a stream's first row group stands for all)
@@ -773,36 +795,36 @@ __global__ void __launch_bounds__(kNoteWarps * 32) kv_weights_kernel(const AttnA
             sum[u] = 0.0f;
         }
 #pragma unroll
-        for (int u = 0; u < kTilesAhead; ++u) old[u] = seg[u] >= 0 ? *to[u] : 0.0f;
+        for (int u = 0; u < N; ++u) old[u] = seg[u] >= 0 ? *to[u] : 0.0f;
         for (int rg = 0; rg < a.row_groups; ++rg) {
-            const float* from[kTilesAhead];
-#pragma unroll
-            for (int u = 0; u < kTilesAhead; ++u) {
-                const int x = seg[u] < 0 ? 0 : rg == 0 ? x0 + u : x0 + u - a.begin[seg[u]] + a.begin[seg[u] + rg];
-                from[u] = a.scores + ((size_t)x * kTile + lane) * ROWS;
-            }
             const int rows = min(ROWS, a.rows - rg * ROWS);
+            float4 s[N][Q], l[N][2 * Q];
 #pragma unroll
-            for (int r = 0; r < ROWS; r += 4) {
-                if (r >= rows) break;
-                float4 s[kTilesAhead];
+            for (int u = 0; u < N; ++u) {
+                const int sg = max(seg[u], 0), x = rg == 0 ? x0 + u : x0 + u - a.begin[sg] + a.begin[sg + rg];
+                const float4* const from = reinterpret_cast<const float4*>(a.scores + ((size_t)(seg[u] < 0 ? 0 : x) * kTile + lane) * ROWS);
+                const float4* const lse = reinterpret_cast<const float4*>(a.lse + (size_t)(sg + rg) * ROWS);
 #pragma unroll
-                for (int u = 0; u < kTilesAhead; ++u) s[u] = seg[u] >= 0 ? *reinterpret_cast<const float4*>(from[u] + r) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int u = 0; u < kTilesAhead; ++u) {
-                    if (seg[u] < 0) continue;
-                    const float e[4] = {s[u].x, s[u].y, s[u].z, s[u].w};
-                    const float4* const lse = reinterpret_cast<const float4*>(a.lse + (size_t)(seg[u] + rg) * ROWS + r);
-                    const float4 l0 = lse[0], l1 = lse[1];
-                    sum[u] = fmaf(exp2_fast(e[0] - l0.x), l0.y, sum[u]);
-                    if (r + 1 < rows) sum[u] = fmaf(exp2_fast(e[1] - l0.z), l0.w, sum[u]);
-                    if (r + 2 < rows) sum[u] = fmaf(exp2_fast(e[2] - l1.x), l1.y, sum[u]);
-                    if (r + 3 < rows) sum[u] = fmaf(exp2_fast(e[3] - l1.z), l1.w, sum[u]);
+                for (int q = 0; q < Q; ++q) {
+                    if (seg[u] < 0 || 4 * q >= rows) continue;
+                    s[u][q] = from[q];
+                    l[u][2 * q] = lse[2 * q], l[u][2 * q + 1] = lse[2 * q + 1];
                 }
             }
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    if (seg[u] < 0 || 4 * q >= rows) continue;
+                    const float4 e = s[u][q], l0 = l[u][2 * q], l1 = l[u][2 * q + 1];
+                    sum[u] = fmaf(exp2_fast(e.x - l0.x), l0.y, sum[u]);
+                    if (4 * q + 1 < rows) sum[u] = fmaf(exp2_fast(e.y - l0.z), l0.w, sum[u]);
+                    if (4 * q + 2 < rows) sum[u] = fmaf(exp2_fast(e.z - l1.x), l1.y, sum[u]);
+                    if (4 * q + 3 < rows) sum[u] = fmaf(exp2_fast(e.w - l1.z), l1.w, sum[u]);
+                }
         }
 #pragma unroll
-        for (int u = 0; u < kTilesAhead; ++u)
+        for (int u = 0; u < N; ++u)
             if (seg[u] >= 0) *to[u] = old[u] + sum[u];
     }
 }
@@ -843,7 +865,7 @@ template <int FMT, int D, int ROWS>
 cudaError_t launch_attention(const AttnArgs& a, cudaStream_t s)
 {
     using S = AttnShape<D, ROWS>;
-    constexpr size_t smem = (size_t)S::kWarps * S::kStages * S::kTileBytes;
+    constexpr size_t smem = (size_t)S::kWarps * S::kStages * S::kTileBytes + (size_t)kMaxAttnCtas * ROWS * sizeof(float2);
     static thread_local int allowed_dev = -1;
     int dev = 0;
     cudaError_t err = cudaGetDevice(&dev);
