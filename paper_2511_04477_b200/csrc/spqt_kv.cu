@@ -37,7 +37,7 @@ __device__ __forceinline__ float quotient_to_odd(float x, float s, float inv)
 }
 
 template <int FMT>
-__device__ __forceinline__ uint2 to_codes(const uint4& h, float s, float inv)
+__device__ __noinline__ uint2 to_codes_exactly(uint4 h, float s, float inv)
 {
     const __half2* p = reinterpret_cast<const __half2*>(&h);
     unsigned w[2] = {0u, 0u};
@@ -54,22 +54,79 @@ __device__ __forceinline__ uint2 to_codes(const uint4& h, float s, float inv)
     return make_uint2(w[0], w[1]);
 }
 
+// Eight values.  x * (1/s) in fp32, within 2^-23 of x/s relative to it, rounds as x/s does unless a tie lies that near: where one of
+// the eight is near a tie the exact steps above are taken for them, which happens for one in hundreds (they are 30 instructions
+// a value, these 6: a prompt's 30 million values 34 us with them alone).
+template <int FMT>
+__device__ __forceinline__ uint2 to_codes(const uint4& h, float s, float inv)
+{
+    const unsigned u[4] = {h.x, h.y, h.z, h.w};
+    unsigned w[2];
+    bool near = false;
+    if (FMT == SPQT_KV_INT8) {
+        constexpr float kMagic = 12582912.0f;   // 1.5 * 2^23: its sum's last bits are the whole number
+        const unsigned long long i2 = pack2(inv, inv), s2 = pack2(-s, -s), m2 = pack2(kMagic, kMagic), n2 = pack2(-kMagic, -kMagic);
+        float far = 0.0f;
+        unsigned t[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+            const unsigned long long x = pack2(f.x, f.y);
+            unsigned long long q = m2, r = x;
+            ffma2(q, x, i2);
+            ffma2(r, fadd2(q, n2), s2);         // what is left of x: exact
+            float lo, hi;
+            unpack2(r, lo, hi);
+            far = fmaxf(far, fmaxf(fabsf(lo), fabsf(hi)));
+            unpack2(q, lo, hi);
+            t[2 * i] = __float_as_uint(lo), t[2 * i + 1] = __float_as_uint(hi);
+        }
+        near = far >= s * 0.49993896484375f;    // 1/2 - 2^-14
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            w[i] = __byte_perm(__byte_perm(t[4 * i], t[4 * i + 1], 0x0040), __byte_perm(t[4 * i + 2], t[4 * i + 3], 0x0040), 0x5410);
+    } else {
+        const unsigned long long i2 = pack2(inv, inv);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            unsigned pair[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[2 * i + k]));
+                float lo, hi;
+                unpack2(fmul2(pack2(f.x, f.y), i2), lo, hi);
+                pair[k] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+                // a tie has 1000... behind the three bits that stay; below 2^-6 fewer stay, and zero is no tie
+                const unsigned a = __float_as_uint(lo) & 0x7fffffffu, b = __float_as_uint(hi) & 0x7fffffffu;
+                near = near || ((a + 0x80008u) & 0xfffffu) < 0x11u || ((b + 0x80008u) & 0xfffffu) < 0x11u || a - 1u < 0x3c800000u - 1u || b - 1u < 0x3c800000u - 1u;
+            }
+            w[i] = pair[0] | pair[1] << 16;
+        }
+    }
+    return near ? to_codes_exactly<FMT>(h, s, inv) : make_uint2(w[0], w[1]);
+}
+
+// Eight codes times their scale, rounded to fp16.
 template <int FMT>
 __device__ __forceinline__ uint4 from_codes(const uint2& w, float s)
 {
-    uint4 h;
-    __half2* p = reinterpret_cast<__half2*>(&h);
+    const unsigned long long s2 = pack2(s, s);
+    unsigned h[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const unsigned pair = (i < 2 ? w.x : w.y) >> (16 * (i & 1)) & 0xffffu;
         float2 f;
-        if (FMT == SPQT_KV_INT8)
-            f = make_float2((float)(signed char)(pair & 0xffu), (float)(signed char)(pair >> 8));
-        else
-            f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
-        p[i] = __floats2half2_rn(f.x * s, f.y * s);
+        if (FMT == SPQT_KV_INT8) {              // code + 128 under the exponent of 1024: 1152 + code
+            const unsigned v = __byte_perm((i < 2 ? w.x : w.y) ^ 0x80808080u, 0x64646464u, i & 1 ? 0x4342 : 0x4140);
+            f = __half22float2(__hsub2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x6480))));
+        } else {
+            f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((i < 2 ? w.x : w.y) >> (16 * (i & 1)) & 0xffffu), __NV_E4M3)));
+        }
+        float lo, hi;
+        unpack2(fmul2(pack2(f.x, f.y), s2), lo, hi);
+        const __half2 r = __floats2half2_rn(lo, hi);
+        h[i] = *reinterpret_cast<const unsigned*>(&r);
     }
-    return h;
+    return make_uint4(h[0], h[1], h[2], h[3]);
 }
 
 // ---------------------------------------------------------------- new tokens
@@ -106,10 +163,24 @@ __global__ void __launch_bounds__(1024) kv_append_kernel(const AppendArgs a)
         refuse(a.status);
         count = 0;
     }
-    const int first = n / bt, before = n % bt;
+    const int shift = 31 - __clz(bt), first = n >> shift, before = n & (bt - 1);
     const long long end = (long long)n + count;
     const int total = before + count;               // rows from the beginning of block `first` on
-    const int touched = (total + bt - 1) / bt;
+    const int touched = (total + bt - 1) >> shift, closed = total >> shift;
+    const bool values = tid >= half;
+    const int t = values ? tid - half : tid;
+    const __half* const fresh = (values ? a.v : a.k) + (long long)b * a.batch_stride + (long long)h * D;
+    __half* const tail = static_cast<__half*>(values ? c.v_tail : c.k_tail) + (size_t)stream * bt * D;
+    constexpr int kRow = D / 8;                     // pieces of a row
+    const int pieces = bt * kRow;
+    // (the rows are on their way while the table is looked at)
+    uint4 x[PPT];
+#pragma unroll
+    for (int i = 0; i < PPT; ++i) {
+        const int p = i * half + t, r = p / kRow, at = j * bt + r - before;
+        const __half* src = at < 0 ? tail + r * D : fresh + (long long)at * a.token_stride;
+        x[i] = ld_global_v4_if(j < closed && p < pieces, src + p % kRow * 8);
+    }
     bool fine = held == n && end <= (long long)c.table_width * bt;
     const int32_t* const row = c.table + (size_t)stream * c.table_width + first;
     if (count > 0) {                                // every CTA of the stream comes to the same verdict
@@ -130,22 +201,8 @@ __global__ void __launch_bounds__(1024) kv_append_kernel(const AppendArgs a)
         const int from = j == 0 ? before : 0, to = min(bt, total - j * bt);
         for (int i = from + tid; i < to; i += blockDim.x) c.weight[block * bt + i] = 0.0f;
     }
-    const bool values = tid >= half;
-    const int t = values ? tid - half : tid;
-    const int closed = total / bt;
-    const __half* const fresh = (values ? a.v : a.k) + (long long)b * a.batch_stride + (long long)h * D;
-    __half* const tail = static_cast<__half*>(values ? c.v_tail : c.k_tail) + (size_t)stream * bt * D;
-    constexpr int kRow = D / 8;                     // pieces of a row
     if (j < closed) {
-        uint4 x[PPT];
         unsigned top = 0u;
-        const int pieces = bt * kRow;
-#pragma unroll
-        for (int i = 0; i < PPT; ++i) {
-            const int p = i * half + t, r = p / kRow, at = j * bt + r - before;
-            const __half* src = at < 0 ? tail + r * D : fresh + (long long)at * a.token_stride;
-            x[i] = ld_global_v4_if(p < pieces, src + p % kRow * 8);
-        }
 #pragma unroll
         for (int i = 0; i < PPT; ++i) {
             // (magnitudes of fp16 in the order of their bits, not-a-number above infinity)
@@ -211,46 +268,64 @@ struct ReadArgs {
     int* status;
 };
 
-constexpr int kReadTokens = 16;   // of a CTA: a part of one block of every stream of a sequence
+constexpr int kReadTokens = 16, kReadWarps = 8;   // of a warp: a part of one block of a stream; of a CTA
 
-// Pieces of eight values, those of a row and then the heads of a token side by side, as the output has them.
+// A warp turns sixteen tokens of a stream, a piece of one block or of the tail; the warps of the heads of the same tokens are
+// neighbours, since their rows are neighbours in the output.
 template <int FMT, int D>
-__global__ void __launch_bounds__(256) kv_read_kernel(const ReadArgs a)
+__global__ void __launch_bounds__(kReadWarps * 32) kv_read_kernel(const ReadArgs a)
 {
     const spqt_kv_cache& c = a.c;
-    constexpr int kRow = D / 8;
-    const int t0 = blockIdx.x * kReadTokens, b = blockIdx.y, bt = c.block_tokens;
+    constexpr int kRow = D / 8, N = kReadTokens * kRow / 32;   // pieces of eight values: of a row, of a lane
+    const int lane = threadIdx.x & 31, w = blockIdx.x * kReadWarps + (threadIdx.x >> 5), b = blockIdx.y;
+    const int h = w % c.kv_heads, t0 = w / c.kv_heads * kReadTokens, bt = c.block_tokens, shift = 31 - __clz(bt), j = t0 >> shift;
+    const int stream = b * c.kv_heads + h;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int per_token = c.kv_heads * kRow;
-#pragma unroll 2
-    for (int i = threadIdx.x; i < kReadTokens * per_token; i += 256) {
-        const int t = t0 + i / per_token, rest = i % per_token, h = rest / kRow, p = rest % kRow;
-        const int stream = b * c.kv_heads + h;
-        const int n = length_or_none(a.length[stream], c, a.status);
-        if (t >= n || t >= a.tokens) continue;
-        uint4 k, v;
-        const int j = t / bt, r = t % bt;
-        if (t < n / bt * bt) {
-            const unsigned block = (unsigned)c.table[(size_t)stream * c.table_width + j];
-            const bool known = block < (unsigned)c.blocks;
-            const size_t id = known ? block : 0u;
-            const size_t at = (id * bt + r) * D + p * 8;
-            float ks = c.k_scale[id], vs = c.v_scale[id];
-            if (!known) {
-                refuse(a.status);
-                ks = vs = __int_as_float(0x7fffffff);
-            }
-            k = from_codes<FMT>(*reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k_codes) + at), ks);
-            v = from_codes<FMT>(*reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v_codes) + at), vs);
-        } else {
-            const size_t at = ((size_t)stream * bt + r) * D + p * 8;
-            k = *reinterpret_cast<const uint4*>(static_cast<const __half*>(c.k_tail) + at);
-            v = *reinterpret_cast<const uint4*>(static_cast<const __half*>(c.v_tail) + at);
+    if (t0 >= a.tokens) return;
+    // (t0 < a.tokens <= table_width * bt: the entry is there, whatever it holds)
+    const unsigned block = (unsigned)c.table[(size_t)stream * c.table_width + j];
+    const int n = length_or_none(a.length[stream], c, a.status), last = min(n, a.tokens);
+    if (t0 >= last) return;
+    long long to = (long long)b * a.batch_stride + (long long)h * a.head_stride;
+    uint4 k[N], v[N];
+    if (t0 < n >> shift << shift) {
+        const bool known = block < (unsigned)c.blocks;
+        const size_t id = known ? block : 0u, at = ((id << shift) + (t0 & (bt - 1))) * D + lane * 8;
+        uint2 kc[N], vc[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            kc[i] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k_codes) + at + i * 256);
+            vc[i] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v_codes) + at + i * 256);
         }
-        const long long to = (long long)b * a.batch_stride + (long long)t * a.token_stride + (long long)h * a.head_stride + p * 8;
-        *reinterpret_cast<uint4*>(a.k + to) = k;
-        *reinterpret_cast<uint4*>(a.v + to) = v;
+        float ks = c.k_scale[id], vs = c.v_scale[id];
+        if (!known) {
+            refuse(a.status);
+            ks = vs = __int_as_float(0x7fffffff);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = i * 32 + lane, t = t0 + p / kRow;
+            if (t >= last) continue;
+            const long long at = to + (long long)t * a.token_stride + p % kRow * 8;
+            *reinterpret_cast<uint4*>(a.k + at) = from_codes<FMT>(kc[i], ks);
+            *reinterpret_cast<uint4*>(a.v + at) = from_codes<FMT>(vc[i], vs);
+        }
+    } else {
+        const size_t at = (((size_t)stream << shift) + (t0 & (bt - 1))) * D + lane * 8;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            k[i] = *reinterpret_cast<const uint4*>(static_cast<const __half*>(c.k_tail) + at + i * 256);
+            v[i] = *reinterpret_cast<const uint4*>(static_cast<const __half*>(c.v_tail) + at + i * 256);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = i * 32 + lane, t = t0 + p / kRow;
+            if (t >= last) continue;
+            const long long at = to + (long long)t * a.token_stride + p % kRow * 8;
+            *reinterpret_cast<uint4*>(a.k + at) = k[i];
+            *reinterpret_cast<uint4*>(a.v + at) = v[i];
+        }
     }
 }
 
@@ -446,7 +521,6 @@ spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void
     if (st != SPQT_OK) return st;
     if (!k || !v || tokens < 1 || batch_stride < 0 || token_stride < 0 || head_stride < 0) return SPQT_ERR_INVALID_ARG;
     if (!aligned(k, 16) || !aligned(v, 16) || batch_stride % 8 || token_stride % 8 || head_stride % 8 || !aligned(length, 4)) return SPQT_ERR_ALIGNMENT;
-    if (cache->kv_heads * (cache->head_dim / 8) > 0x7fffffff / kReadTokens) return SPQT_ERR_UNSUPPORTED;
     st = check_kv_workspace(workspace, workspace_bytes, kKvHeader);
     if (st != SPQT_OK) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -454,8 +528,10 @@ spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void
     if (tokens > most) tokens = most;
     const ReadArgs a = {*cache, length ? length : cache->length, static_cast<__half*>(k), static_cast<__half*>(v), tokens, batch_stride, token_stride,
                         head_stride, static_cast<int*>(status_word(workspace))};
-    const dim3 grid((unsigned)((tokens + kReadTokens - 1) / kReadTokens), (unsigned)cache->batch);
-#define SPQT_F(F, D) launch_overlapping(kv_read_kernel<F, D>, grid, 256, 0, s, a)
+    // (warps: at most 2^17 pieces of a row of the table times 2^14 streams)
+    const long long warps = (long long)((tokens + kReadTokens - 1) / kReadTokens) * cache->kv_heads;
+    const dim3 grid((unsigned)((warps + kReadWarps - 1) / kReadWarps), (unsigned)cache->batch);
+#define SPQT_F(F, D) launch_overlapping(kv_read_kernel<F, D>, grid, kReadWarps * 32, 0, s, a)
     const cudaError_t err = SPQT_KV_DISPATCH(*cache, SPQT_F);
 #undef SPQT_F
     return launched(err);
