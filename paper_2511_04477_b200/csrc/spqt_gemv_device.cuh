@@ -286,6 +286,14 @@ __device__ __forceinline__ void ffma2(unsigned long long& d, unsigned long long 
     asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b));
 }
 
+// a * b + c on both lanes
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c)
+{
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
 // d = a * b on both lanes
 __device__ __forceinline__ unsigned long long fmul2(unsigned long long a, unsigned long long b)
 {

@@ -72,9 +72,7 @@ __device__ __forceinline__ uint2 to_codes(const uint4& h, float s, float inv)
         for (int i = 0; i < 4; ++i) {
             const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
             const unsigned long long x = pack2(f.x, f.y);
-            unsigned long long q = m2, r = x;
-            ffma2(q, x, i2);
-            ffma2(r, fadd2(q, n2), s2);         // what is left of x: exact
+            const unsigned long long q = fma2(x, i2, m2), r = fma2(fadd2(q, n2), s2, x);   // r, what is left of x, is exact
             float lo, hi;
             unpack2(r, lo, hi);
             far = fmaxf(far, fmaxf(fabsf(lo), fabsf(hi)));
@@ -145,13 +143,13 @@ struct AppendArgs {
     int* status;
 };
 
-template <int FMT, int D, int PPT>
-__global__ void __launch_bounds__(1024) kv_append_kernel(const AppendArgs a)
+template <int FMT, int D, int PPT, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : 1) kv_append_kernel(const AppendArgs a)
 {
     __shared__ unsigned s_max[32];
     const spqt_kv_cache& c = a.c;
     const int tid = threadIdx.x, half = blockDim.x >> 1, warp = tid >> 5;
-    const int h = blockIdx.x % c.kv_heads, j = blockIdx.x / c.kv_heads, b = blockIdx.y;
+    const int h = blockIdx.x, j = blockIdx.y, b = blockIdx.z;
     const int stream = b * c.kv_heads + h, bt = c.block_tokens;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -172,14 +170,15 @@ __global__ void __launch_bounds__(1024) kv_append_kernel(const AppendArgs a)
     const __half* const fresh = (values ? a.v : a.k) + (long long)b * a.batch_stride + (long long)h * D;
     __half* const tail = static_cast<__half*>(values ? c.v_tail : c.k_tail) + (size_t)stream * bt * D;
     constexpr int kRow = D / 8;                     // pieces of a row
-    const int pieces = bt * kRow;
+    const int r0 = t / kRow, col = t % kRow * 8, step = half / kRow;   // a thread's pieces lie `step` rows apart (half is a multiple of kRow)
     // (the rows are on their way while the table is looked at)
     uint4 x[PPT];
+    const __half* src = fresh + (long long)(j * bt + r0 - before) * a.token_stride + col;
 #pragma unroll
     for (int i = 0; i < PPT; ++i) {
-        const int p = i * half + t, r = p / kRow, at = j * bt + r - before;
-        const __half* src = at < 0 ? tail + r * D : fresh + (long long)at * a.token_stride;
-        x[i] = ld_global_v4_if(j < closed && p < pieces, src + p % kRow * 8);
+        const int r = r0 + i * step;
+        x[i] = ld_global_v4_if(j < closed && r < bt, j * bt + r < before ? tail + r * D + col : src);
+        src += step * a.token_stride;
     }
     bool fine = held == n && end <= (long long)c.table_width * bt;
     const int32_t* const row = c.table + (size_t)stream * c.table_width + first;
@@ -215,14 +214,15 @@ __global__ void __launch_bounds__(1024) kv_append_kernel(const AppendArgs a)
         for (int w = 0; w < half >> 5; ++w) top = max(top, s_max[w0 + w]);
         const bool poisoned = top >= 0x7c00u;
         const float amax = __half2float(__ushort_as_half((unsigned short)top));
-        const float s = poisoned ? __int_as_float(0x7fffffff) : __fdiv_rn(amax, FMT == SPQT_KV_INT8 ? 127.0f : 448.0f);
-        const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+        // amax / 127 or 448, correctly rounded: the quotient by the reciprocal, and what it leaves (every fp16 value has been tried)
+        constexpr float kMost = FMT == SPQT_KV_INT8 ? 127.0f : 448.0f, kInv = 1.0f / kMost;
+        const float q = amax * kInv, exact = fmaf(fmaf(-q, kMost, amax), kInv, q);
+        const float s = poisoned ? __int_as_float(0x7fffffff) : exact;
+        const float inv = s > 0.0f ? __fdividef(1.0f, s) : 0.0f;
         uint2* const dst = reinterpret_cast<uint2*>(static_cast<unsigned char*>(values ? c.v_codes : c.k_codes) + block * bt * D);
 #pragma unroll
-        for (int i = 0; i < PPT; ++i) {
-            const int p = i * half + t;
-            if (p < pieces) dst[p] = poisoned ? make_uint2(0u, 0u) : to_codes<FMT>(x[i], s, inv);
-        }
+        for (int i = 0; i < PPT; ++i)
+            if (r0 + i * step < bt) dst[i * half + t] = poisoned ? make_uint2(0u, 0u) : to_codes<FMT>(x[i], s, inv);
         if (t == 0) (values ? c.v_scale : c.k_scale)[block] = s;
     }
     if (j != 0) return;
@@ -248,13 +248,17 @@ template <int FMT, int D>
 cudaError_t launch_append(const AppendArgs& a, cudaStream_t s)
 {
     const int bt = a.c.block_tokens, pieces = bt * D / 8;
-    const int touched = (int)(((long long)a.tokens + 2 * bt - 2) / bt);
-    const dim3 grid((unsigned)(touched * a.c.kv_heads), (unsigned)a.c.batch);
+    // (blocks behind the table's last are refused by the first CTA of the stream)
+    const int touched = (int)(((long long)a.tokens + 2 * bt - 2) / bt), most = a.c.table_width;
+    const dim3 grid((unsigned)a.c.kv_heads, (unsigned)(touched < most ? touched : most), (unsigned)a.c.batch);
+    // threads for one of k and v: a multiple of a warp and of a row's pieces
+    constexpr int kUnit = D == 96 ? 96 : 32;
     if (pieces <= 2048) {
-        const int half = (pieces / 4 + 31) / 32 * 32;
-        return launch_overlapping(kv_append_kernel<FMT, D, 4>, grid, 2 * half, 0, s, a);
+        const int half = (pieces / 4 + kUnit - 1) / kUnit * kUnit;
+        if (half <= 128) return launch_overlapping(kv_append_kernel<FMT, D, 4, 256>, grid, 2 * half, 0, s, a);
+        return launch_overlapping(kv_append_kernel<FMT, D, 4, 1024>, grid, 2 * half, 0, s, a);
     }
-    return launch_overlapping(kv_append_kernel<FMT, D, 8>, grid, 1024, 0, s, a);
+    return launch_overlapping(kv_append_kernel<FMT, D, 8, 1024>, grid, 1024, 0, s, a);
 }
 
 // ---------------------------------------------------------------- the cache as fp16
@@ -493,8 +497,7 @@ spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void
     if (st != SPQT_OK) return st;
     if (!k || !v || tokens < 1 || batch_stride < 0 || token_stride < 0) return SPQT_ERR_INVALID_ARG;
     if (!aligned(k, 16) || !aligned(v, 16) || batch_stride % 8 || token_stride % 8 || !aligned(counts, 4) || !aligned(length_out, 4)) return SPQT_ERR_ALIGNMENT;
-    if (cache->batch > 65535 || tokens > (1 << 28) || ((long long)tokens + 2 * cache->block_tokens) / cache->block_tokens * cache->kv_heads >= 0x7fffffffLL)
-        return SPQT_ERR_UNSUPPORTED;
+    if (tokens > (1 << 28)) return SPQT_ERR_UNSUPPORTED;
     st = check_kv_workspace(workspace, workspace_bytes, kKvScratch + kv_lengths_bytes(*cache));
     if (st != SPQT_OK) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
