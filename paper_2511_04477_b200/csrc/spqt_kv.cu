@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv_read_kernel(const ReadArgs
 
 // ---------------------------------------------------------------- eviction
 
-constexpr int kEvictThreads = 512, kEvictWarps = kEvictThreads / 32;
+constexpr int kMostEvictWarps = 32;
 
 struct EvictArgs {
     spqt_kv_cache c;
@@ -355,57 +355,57 @@ __device__ __forceinline__ unsigned ordered(float f)
 // How many of the CTA's values are true, and how many are in threads before this one (in thread order).
 __device__ __forceinline__ int count_before(bool v, int* s_warps, int* all)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const unsigned mask = __ballot_sync(0xffffffffu, v);
     __syncthreads();                        // (s_warps may still be read)
     if (lane == 0) s_warps[warp] = __popc(mask);
     __syncthreads();
-    const int mine = lane < kEvictWarps ? s_warps[lane] : 0;
+    const int mine = lane < warps ? s_warps[lane] : 0;
     *all = __reduce_add_sync(0xffffffffu, mine);
     return __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0) + __popc(mask & ((1u << lane) - 1u));
 }
 
-// One CTA per stream: the blocks' sums as ordered whole numbers in shared memory beside the row of the table; the m-th largest by
-// two bits a round; then one pass in order.  The weights are read once; the rest is latency.
-__global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs a)
+// One CTA per stream: the blocks' sums as ordered whole numbers in shared memory beside the row of the table; the m-th largest bit
+// by bit, by a count of the CTA's threads a bit; then one pass in order.  The weights are read once, all loads of a row of up to
+// 32 K tokens in flight together; the rest is a chain of barriers (sixteen streams of 32768 tokens, two bits a round with counts
+// through shared memory and loads in four turns: 17.3 us).
+__global__ void __launch_bounds__(1024) kv_evict_kernel(const EvictArgs a)
 {
     extern __shared__ unsigned s_dyn[];     // keys [table_width], then the row of the table [table_width]
-    __shared__ int s_count[16][3], s_warps[kEvictWarps];
+    __shared__ int s_warps[kMostEvictWarps], s_count;
     const spqt_kv_cache& c = a.c;
-    const int stream = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int bt = c.block_tokens, width = c.table_width;
+    const int stream = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
+    const int bt = c.block_tokens, width = c.table_width, shift = 31 - __clz(bt);
     unsigned* const s_key = s_dyn;
     int* const s_row = reinterpret_cast<int*>(s_dyn + width);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int held = (int)ld_global_u32(c.length + stream);
-    const int n = length_or_none(held, c, a.status);
     const int32_t* const row = c.table + (size_t)stream * width;
     int32_t* const row_out = (a.table_out ? a.table_out : c.table) + (size_t)stream * width;
     int32_t* const length_out = (a.length_out ? a.length_out : c.length) + stream;
-    const int closed = n / bt;
+    for (int i = tid; i < width; i += threads) s_row[i] = row[i];
+    const int n = length_or_none(held, c, a.status);
+    const int closed = n >> shift;
+    __syncthreads();                        // (also: every thread has the length)
     if (closed <= a.keep) {
         if (row_out != row)
-            for (int i = tid; i < width; i += kEvictThreads) row_out[i] = row[i];
+            for (int i = tid; i < width; i += threads) row_out[i] = s_row[i];
         if (tid == 0) *length_out = held;
         return;
     }
-    for (int i = tid; i < width; i += kEvictThreads) s_row[i] = row[i];
-    if (tid < 48) s_count[tid / 3][tid % 3] = 0;
-    __syncthreads();
     // sums: bt / 4 lanes a block, four weights a lane, in fp64 (the order of the sum is then of no consequence to the rounded one
     // but in one case of 2^29)
     const int lanes = bt >> 2, at_once = 32 / lanes, sub = lane / lanes, l = lane % lanes;
-    constexpr int kU = 4;
-    for (int j0 = warp * at_once * kU; j0 < closed; j0 += kEvictWarps * at_once * kU) {
+    constexpr int kU = 8;
+    for (int j0 = warp * at_once * kU; j0 < closed; j0 += (threads >> 5) * at_once * kU) {
         float4 w[kU];
-        bool known[kU];
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             const int j = j0 + u * at_once + sub;
-            const unsigned id = j < closed ? (unsigned)s_row[j] : 0u;
-            known[u] = id < (unsigned)c.blocks;
-            w[u] = j < closed && known[u] ? *reinterpret_cast<const float4*>(c.weight + (size_t)id * bt + 4 * l) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const unsigned id = j < closed ? (unsigned)s_row[j] : 0xffffffffu;
+            w[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (id < (unsigned)c.blocks) w[u] = *reinterpret_cast<const float4*>(c.weight + ((size_t)id << shift) + 4 * l);
         }
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
@@ -413,8 +413,9 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs
             double v = ((double)w[u].x + w[u].y) + ((double)w[u].z + w[u].w);
             for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
             if (l == 0 && j < closed) {
-                s_key[j] = known[u] ? ordered((float)v) : 0u;      // (what no block stands behind leaves first)
-                if (!known[u]) refuse(a.status);
+                const bool known = (unsigned)s_row[j] < (unsigned)c.blocks;
+                s_key[j] = known ? ordered((float)v) : 0u;         // (what no block stands behind leaves first)
+                if (!known) refuse(a.status);
             }
         }
     }
@@ -422,56 +423,64 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const EvictArgs
     // the m-th largest key among the blocks that are not protected
     const int lo = a.first, hi = closed - a.recent, m = a.keep - a.first - a.recent;
     unsigned key = 0u;                      // its bits so far
-    int above = 0;                          // keys above all that share these bits
+    int equal = m;                          // of the keys equal to it only the first so many stay
+    bool exactly = false;                   // m keys reach it, so that all that do stay
     if (m > 0) {
-        for (int round = 0; round < 16; ++round) {
-            const int shift = 30 - 2 * round;
-            const unsigned t1 = key | 1u << shift, t2 = key | 2u << shift, t3 = key | 3u << shift;
-            int c1 = 0, c2 = 0, c3 = 0;
-            for (int j = lo + tid; j < hi; j += kEvictThreads) {
-                const unsigned k = s_key[j];
-                c1 += k >= t1, c2 += k >= t2, c3 += k >= t3;
+        constexpr int kOwn = 4;             // keys of a thread that it keeps in registers; beyond, counts go by way of shared memory
+        const int mine = (hi - lo + threads - 1) / threads;
+        unsigned k[kOwn];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) k[i] = lo + i * threads + tid < hi ? s_key[lo + i * threads + tid] : 0u;   // (0 reaches no trial)
+        auto reach = [&](unsigned trial) {  // how many keys do, in every thread
+            if (mine <= kOwn) {
+                int all = __syncthreads_count(k[0] >= trial);
+#pragma unroll
+                for (int i = 1; i < kOwn; ++i)
+                    if (i < mine) all += __syncthreads_count(k[i] >= trial);
+                return all;
             }
-            c1 = __reduce_add_sync(0xffffffffu, c1), c2 = __reduce_add_sync(0xffffffffu, c2), c3 = __reduce_add_sync(0xffffffffu, c3);
-            if (lane == 0) {
-                if (c1) atomicAdd(&s_count[round][0], c1);
-                if (c2) atomicAdd(&s_count[round][1], c2);
-                if (c3) atomicAdd(&s_count[round][2], c3);
-            }
+            int v = 0;
+            for (int j = lo + tid; j < hi; j += threads) v += s_key[j] >= trial;
+            v = __reduce_add_sync(0xffffffffu, v);
             __syncthreads();
-            const int a1 = s_count[round][0], a2 = s_count[round][1], a3 = s_count[round][2];
-            key = a3 >= m ? t3 : a2 >= m ? t2 : a1 >= m ? t1 : key;
-            if (a3 == m || a2 == m || a1 == m) break;   // these m and no other reach `key`
+            if (tid == 0) s_count = 0;
+            __syncthreads();
+            if (lane == 0) atomicAdd(&s_count, v);
+            __syncthreads();
+            return s_count;
+        };
+        for (int bit = 31; bit >= 0 && !exactly; --bit) {
+            const unsigned trial = key | 1u << bit;
+            const int all = reach(trial);
+            if (all >= m) key = trial;
+            exactly = all == m;
         }
-        int more = 0;
-        for (int j = lo + tid; j < hi; j += kEvictThreads) more += s_key[j] > key;
-        more = __reduce_add_sync(0xffffffffu, more);
-        __syncthreads();
-        if (lane == 0) s_warps[warp] = more;
-        __syncthreads();
-        for (int w = 0; w < kEvictWarps; ++w) above += s_warps[w];
+        if (!exactly && key != 0xffffffffu) equal = m - reach(key + 1u);
     }
     // in order: blocks that stay to the front, the open one, those that leave, the rest where it was
-    const int some = n % bt ? 1 : 0;
-    int equal = m - above, stay = 0, leave = a.keep + some;   // places: of the equal ones only the first `equal` stay
-    for (int j0 = 0; j0 < closed; j0 += kEvictThreads) {
+    const int some = n & (bt - 1) ? 1 : 0;
+    int stay = 0, leave = a.keep + some;    // places
+    for (int j0 = 0; j0 < closed; j0 += threads) {
         const int j = j0 + tid;
         const bool in = j >= lo && j < hi;
         const unsigned k = in ? s_key[j] : 0u;
         int all;
-        const bool same = in && m > 0 && k == key;
-        const int rank = count_before(same, s_warps, &all);
-        const bool keeps = j < closed && (!in || (m > 0 && (k > key || (same && rank < equal))));
-        equal -= all;
+        bool keeps = j < closed && (!in || (m > 0 && k >= key));
+        if (!exactly) {
+            const bool same = in && m > 0 && k == key;
+            const int rank = count_before(same, s_warps, &all);
+            keeps = keeps && !(same && rank >= equal);
+            equal -= all;
+        }
         const int place = count_before(keeps, s_warps, &all);
         if (j < closed) row_out[keeps ? stay + place : leave + tid - place] = s_row[j];
         stay += all;
-        leave += min(kEvictThreads, closed - j0) - all;
+        leave += min(threads, closed - j0) - all;
     }
     if (some && tid == 0) row_out[a.keep] = s_row[closed];
     if (row_out != row)
-        for (int i = closed + some + tid; i < width; i += kEvictThreads) row_out[i] = s_row[i];
-    if (tid == 0) *length_out = a.keep * bt + n % bt;
+        for (int i = closed + some + tid; i < width; i += threads) row_out[i] = s_row[i];
+    if (tid == 0) *length_out = a.keep * bt + (n & (bt - 1));
 }
 
 }  // namespace spqt
@@ -560,7 +569,9 @@ spqt_status spqt_kv_evict(const spqt_kv_cache* cache, int keep, int first, int r
         allowed_dev = dev;
     }
     const EvictArgs a = {*cache, keep, first, recent, table_out, length_out, static_cast<int*>(status_word(workspace))};
-    return launched(launch_overlapping(kv_evict_kernel, dim3(cache->batch * cache->kv_heads), kEvictThreads, smem, static_cast<cudaStream_t>(stream), a));
+    // a thread per block of a row, and some more for the loads of short ones
+    const int threads = cache->table_width <= 128 ? 128 : cache->table_width <= 512 ? 512 : 1024;
+    return launched(launch_overlapping(kv_evict_kernel, dim3(cache->batch * cache->kv_heads), threads, smem, static_cast<cudaStream_t>(stream), a));
 }
 
 spqt_status spqt_kv_status(const void* workspace, int* status_host, void* stream)
