@@ -336,6 +336,7 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv_read_kernel(const ReadArgs
 // ---------------------------------------------------------------- eviction
 
 constexpr int kMostEvictWarps = 32;
+constexpr int kOwnKeys = 32;      // keys of a lane, where one warp looks for the bound
 
 struct EvictArgs {
     spqt_kv_cache c;
@@ -366,13 +367,13 @@ __device__ __forceinline__ int count_before(bool v, int* s_warps, int* all)
 }
 
 // One CTA per stream: the blocks' sums as ordered whole numbers in shared memory beside the row of the table; the m-th largest bit
-// by bit, by a count of the CTA's threads a bit; then one pass in order.  The weights are read once, all loads of a row of up to
-// 32 K tokens in flight together; the rest is a chain of barriers (sixteen streams of 32768 tokens, two bits a round with counts
-// through shared memory and loads in four turns: 17.3 us).
+// by bit; then one pass in order.  The weights are read once, all loads of a row of up to 32 K tokens in flight together; the rest is
+// a chain of steps.  Up to 1024 keys are one warp's, without a barrier of the CTA for every bit: that takes 0.2 to 0.3 us, by
+// __syncthreads_count as by counts in shared memory (sixteen times 32768 tokens 13.8 and 17.3 us).
 __global__ void __launch_bounds__(1024) kv_evict_kernel(const EvictArgs a)
 {
     extern __shared__ unsigned s_dyn[];     // keys [table_width], then the row of the table [table_width]
-    __shared__ int s_warps[kMostEvictWarps], s_count;
+    __shared__ int s_warps[kMostEvictWarps], s_found[3];
     const spqt_kv_cache& c = a.c;
     const int stream = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
     const int bt = c.block_tokens, width = c.table_width, shift = 31 - __clz(bt);
@@ -407,14 +408,18 @@ __global__ void __launch_bounds__(1024) kv_evict_kernel(const EvictArgs a)
             w[u] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (id < (unsigned)c.blocks) w[u] = *reinterpret_cast<const float4*>(c.weight + ((size_t)id << shift) + 4 * l);
         }
+        double v[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) v[u] = ((double)w[u].x + w[u].y) + ((double)w[u].z + w[u].w);
+        for (int o = 1; o < lanes; o <<= 1)
+#pragma unroll
+            for (int u = 0; u < kU; ++u) v[u] += __shfl_xor_sync(0xffffffffu, v[u], o);
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             const int j = j0 + u * at_once + sub;
-            double v = ((double)w[u].x + w[u].y) + ((double)w[u].z + w[u].w);
-            for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
             if (l == 0 && j < closed) {
                 const bool known = (unsigned)s_row[j] < (unsigned)c.blocks;
-                s_key[j] = known ? ordered((float)v) : 0u;         // (what no block stands behind leaves first)
+                s_key[j] = known ? ordered((float)v[u]) : 0u;      // (what no block stands behind leaves first)
                 if (!known) refuse(a.status);
             }
         }
@@ -425,29 +430,44 @@ __global__ void __launch_bounds__(1024) kv_evict_kernel(const EvictArgs a)
     unsigned key = 0u;                      // its bits so far
     int equal = m;                          // of the keys equal to it only the first so many stay
     bool exactly = false;                   // m keys reach it, so that all that do stay
-    if (m > 0) {
-        constexpr int kOwn = 4;             // keys of a thread that it keeps in registers; beyond, counts go by way of shared memory
-        const int mine = (hi - lo + threads - 1) / threads;
-        unsigned k[kOwn];
+    if (m > 0 && hi - lo <= 32 * kOwnKeys) {   // the first warp alone, which keeps the keys in registers
+        if (warp == 0) {
+            const int mine = (hi - lo + 31) / 32;
+            unsigned k[kOwnKeys];
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) k[i] = lo + i * threads + tid < hi ? s_key[lo + i * threads + tid] : 0u;   // (0 reaches no trial)
-        auto reach = [&](unsigned trial) {  // how many keys do, in every thread
-            if (mine <= kOwn) {
-                int all = __syncthreads_count(k[0] >= trial);
+            for (int i = 0; i < kOwnKeys; ++i) k[i] = lo + i * 32 + lane < hi ? s_key[lo + i * 32 + lane] : 0u;   // (0 reaches no trial)
+            auto reach = [&](unsigned trial) {
+                int v = 0;
 #pragma unroll
-                for (int i = 1; i < kOwn; ++i)
-                    if (i < mine) all += __syncthreads_count(k[i] >= trial);
-                return all;
+                for (int i = 0; i < kOwnKeys / 4; ++i) v += k[i] >= trial;
+                if (mine > kOwnKeys / 4) {
+#pragma unroll
+                    for (int i = kOwnKeys / 4; i < kOwnKeys; ++i) v += k[i] >= trial;
+                }
+                return __reduce_add_sync(0xffffffffu, v);
+            };
+            for (int bit = 31; bit >= 0 && !exactly; --bit) {
+                const unsigned trial = key | 1u << bit;
+                const int all = reach(trial);
+                if (all >= m) key = trial;
+                exactly = all == m;
             }
+            if (!exactly && key != 0xffffffffu) equal = m - reach(key + 1u);
+            if (lane == 0) s_found[0] = (int)key, s_found[1] = equal, s_found[2] = exactly;
+        }
+        __syncthreads();
+        key = (unsigned)s_found[0], equal = s_found[1], exactly = s_found[2] != 0;
+    } else if (m > 0) {
+        auto reach = [&](unsigned trial) {  // how many keys do, in every thread
             int v = 0;
             for (int j = lo + tid; j < hi; j += threads) v += s_key[j] >= trial;
             v = __reduce_add_sync(0xffffffffu, v);
             __syncthreads();
-            if (tid == 0) s_count = 0;
+            if (tid == 0) s_found[0] = 0;
             __syncthreads();
-            if (lane == 0) atomicAdd(&s_count, v);
+            if (lane == 0) atomicAdd(&s_found[0], v);
             __syncthreads();
-            return s_count;
+            return s_found[0];
         };
         for (int bit = 31; bit >= 0 && !exactly; --bit) {
             const unsigned trial = key | 1u << bit;
