@@ -2,7 +2,7 @@
 """Benchmark of the SpQt hot path on B200: one line of JSON on stdout.
 
     python bench.py [--gpus N] [--steps K] [--warmup W]            the headline line (config "layer")
-    python bench.py --config sweep | formats | dense | batch | kquant | models | stack   the other workloads, one JSON line each
+    python bench.py --config sweep | formats | dense | batch | kquant | models | stack | decode   the other workloads, one JSON line each
     python bench.py --impl reference                               the fp64 CPU oracle on a bounded sample
 
 Workload of the headline line (the configuration the metric is quoted on): the seven linear layers of
@@ -306,6 +306,15 @@ def other_config_line(which, local, quick=False):
                                             "fresh x per token; one CUDA graph per token (128 launches, index collection inside)"},
                         roofline=roofline_obj(res["needed_gbs"], peak, kind, nb, res["ms_per_token"] * 1e3 / res["launches_per_token"],
                                               "gemv_kernel<128,4,fused>"),
+                        result=res)
+        elif which == "decode":
+            res = sweep.run_decode(layers=8 if quick else 32, peak=peak)
+            line = dict(base, metric="tokens/s of whole decode steps, 32-layer Llama-3-8B-shaped stack, int4 g128, 40% sparsity, 8-bit cache bounded "
+                                     "by accumulated attention",
+                        unit="tokens/s", value=res["tokens_per_s"], ms_per_step=res["ms_per_token"], steps=res["tokens"], warmup=32,
+                        config={"workload": "%d layers x (q|k|v, cache append, attention with weights, o, gate|up, down), dense head 128256x4096 and log "
+                                            "probabilities; context 8192, cut to 2048 tokens' blocks of 32 with every full block; one CUDA graph per kind of token"
+                                            % res["layers"]},
                         result=res)
         else:
             raise SystemExit("unknown --config %r" % which)
@@ -691,7 +700,7 @@ def main():
     ap.add_argument("--steps", type=int, default=1024)
     ap.add_argument("--warmup", type=int, default=8)
     ap.add_argument("--impl", default="ours", choices=["ours", "reference"])
-    ap.add_argument("--config", default="layer", choices=["layer", "sweep", "formats", "dense", "batch", "kquant", "models", "stack"])
+    ap.add_argument("--config", default="layer", choices=["layer", "sweep", "formats", "dense", "batch", "kquant", "models", "stack", "decode"])
     ap.add_argument("--min-seconds", type=float, default=MIN_TIMED_S,
                     help="device time to accumulate over repeated K-step regions of the headline measurement")
     ap.add_argument("--quick", action="store_true", help="reduced form of --config sweep/formats/stack")

@@ -1,6 +1,6 @@
-"""The benchmark's other workloads: sparsity sweep, format sweep, dense shape sweep and the 32-layer stack.
+"""The benchmark's other workloads: sparsity sweep, format sweep, dense shape sweep, the 32-layer stack and its whole decode steps.
 
-Used by ``bench.py --config sweep|formats|dense|stack`` (and, in reduced form, by its default line).
+Used by ``bench.py --config sweep|formats|dense|stack|decode`` (and, in reduced form, by its default line).
 Each case packs several distinct weight copies (together well above the 126 MB L2), visits them
 round-robin inside one CUDA graph and times graph replays with CUDA events on the launching stream.
 Weights are random-init on the device (their values do not affect timing); x and thresholds come
@@ -391,5 +391,105 @@ def run_stack(layers=32, tokens=100, peak=None):
            "packed_gb": sum(p.nbytes for row in packs for p in row.values()) * 1e-9,
            "device_status": status}
     del packs, graphs
+    torch.cuda.empty_cache()
+    return out
+
+
+DECODE_HEADS = dict(q_heads=32, kv_heads=8, head_dim=128)   # of the stack's layers: q | k | v are 4096 + 1024 + 1024 rows
+DECODE_VOCAB = 128256
+
+
+def run_decode(layers=32, context=8192, keep=2048, tokens=96, block=32, sparsity=0.4, peak=None):
+    """Whole decode steps of the stack at batch 1: in every layer q | k | v, the new key and value into the layer's 8-bit cache,
+    attention over it with the weights accumulated, o, gate | up and down, then the head (dense) and the log probability, entropy
+    and alternatives of the token.  The cache holds `context` tokens at the beginning and between `keep` and `keep` plus
+    a block afterwards: with every block that becomes full all but the `keep` tokens' blocks of largest accumulated weight leave
+    (the first and the last four always stay).  One graph per kind of token, replayed; lengths and tables live on the device, so
+    that a replay is the next token."""
+    peak = peak or hbm_peak()[0]
+    H, KV, D = (DECODE_HEADS[k] for k in ("q_heads", "kv_heads", "head_dim"))
+    packs, thr, xs = build_stack(layers, 1, sparsity)
+    head = make_copies(DECODE_VOCAB, 4096, 4, 128, 1, seed0=10000)[0]
+    ws = {site: binding.new_workspace(m, n, 4, 128) for (site, m, n, _) in STACK_SITES}
+    ws_head = binding.new_workspace(DECODE_VOCAB, 4096, 4, 128)
+    dev = {"device": "cuda"}
+    width = context // block + 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(31)
+    caches = []
+    for L in range(layers):
+        c = binding.KVCache.new(1, KV, D, block, KV * width, width, weight=True)
+        c.table.copy_(torch.randperm(KV * width, generator=g, **dev).int().view(1, KV, width))
+        caches.append(c)
+    kv_ws = binding.new_kv_workspace(caches[0], H)
+    for c in caches:                                    # the context, as a prompt leaves it
+        k, v = (torch.randn((1, context - 1, KV, D), generator=g, **dev).half() for _ in range(2))
+        binding.spqt_kv_append(c, k, v, kv_ws)
+    y = {site: torch.empty(m, dtype=torch.float16, **dev) for (site, m, n, _) in STACK_SITES}
+    idx = {site: torch.empty(n, dtype=torch.int32, **dev) for (site, m, n, _) in STACK_SITES}
+    cnt = {site: torch.zeros(1, dtype=torch.int32, **dev) for (site, m, n, _) in STACK_SITES}
+    att = torch.empty((1, 1, H, D), dtype=torch.float16, **dev)
+    logits = torch.empty((1, DECODE_VOCAB), dtype=torch.float16, **dev)
+    token = torch.zeros(1, dtype=torch.int32, **dev)
+    x = {site: xs[site][1][0] for (site, m, n, _) in STACK_SITES}
+    x["attn_out"] = att.view(-1)
+    rows = y["attn_in"].view(1, 1, -1, D)               # the heads of q, k and v side by side
+    answers = []
+
+    def linear(L, site, t, stream):
+        binding.spqt_sparsify_gemv(packs[L][site], x[site], t, ws[site], idx[site], cnt[site], y[site], stream=stream)
+
+    def step(stream, evict, attn_out_thr):
+        for L in range(layers):
+            linear(L, "attn_in", thr["attn_in"], stream)
+            binding.spqt_kv_append(caches[L], rows[:, :, H:H + KV], rows[:, :, H + KV:], kv_ws, stream=stream)
+            binding.spqt_kv_attention(caches[L], rows[:, :, :H], kv_ws, accumulate=True, out=att, stream=stream)
+            if evict:
+                binding.spqt_kv_evict(caches[L], keep // block, kv_ws, first=1, recent=min(4, keep // block // 2), stream=stream)
+            linear(L, "attn_out", attn_out_thr[L], stream)
+            linear(L, "mlp_in", thr["mlp_in"], stream)
+            linear(L, "mlp_mid", thr["mlp_mid"], stream)
+        binding.spqt_dense_gemv(head, y["attn_out"], ws_head, logits.view(-1), stream=stream)
+        answers[:] = binding.spqt_token_logprobs(logits, token, top=5, stream=stream)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        # thresholds of o's input, which here is the attention's own output
+        attn_out_thr = []
+        for L in range(layers):
+            linear(L, "attn_in", thr["attn_in"], s)
+            binding.spqt_kv_attention(caches[L], rows[:, :, :H], kv_ws, out=att, stream=s)
+            attn_out_thr.append(float(binding.spqt_calibrate_threshold(att.view(-1), sparsity, stream=s)))
+        step(s, True, attn_out_thr)                      # the token that fills the context's last block; down to the budget
+    torch.cuda.synchronize()
+    graphs = []
+    for evict in (False, True):
+        gph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gph, stream=s):
+            step(s, evict, attn_out_thr)
+        graphs.append((gph, answers[:]))
+    tokens = max(block, tokens // block * block)
+    e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    with torch.cuda.stream(s):
+        for i in range(block):                           # warm-up: a block's tokens
+            graphs[i % block == block - 1][0].replay()
+        e[0].record(s)
+        for i in range(tokens):
+            graphs[i % block == block - 1][0].replay()
+        e[1].record(s)
+        e[1].synchronize()
+    ms = e[0].elapsed_time(e[1]) / tokens
+    n = [int(c.length.max()) for c in caches]
+    status = max([binding.spqt_workspace_status(ws[site], m, 128) for (site, m, n_, _) in STACK_SITES] + [binding.spqt_kv_status(kv_ws)])
+    logprob, entropy, top, index = graphs[1][1]
+    cached = keep + block / 2
+    read = layers * KV * cached * (2 * D + 8 + 12 / block)
+    out = {"layers": layers, "context": context, "budget_tokens": keep, "tokens": tokens, "ms_per_token": ms, "tokens_per_s": 1e3 / ms,
+           "launches_per_token": layers * (4 + 3 + 1 / block) + 2, "cache_mb_read_per_token": read * 1e-6,
+           "cache_bytes_per_token_of_context": 2 * D * KV * layers, "length": max(n), "logprob": float(logprob[0]), "entropy": float(entropy[0]),
+           "top_index": index[0].tolist(), "device_status": status}
+    assert min(n) == max(n) == keep, n
+    del packs, graphs, caches, head
     torch.cuda.empty_cache()
     return out
