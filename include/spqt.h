@@ -6,7 +6,9 @@
  * state entries whose magnitude exceeds a calibrated threshold, (2) multiply
  * only the matching columns of the group-quantized W, which is stored in the
  * "zigzag" layout so that a skipped column is a run of whole quantization
- * blocks.  This library is that path and nothing else.
+ * blocks.  This library is that path, and what a decode step needs beside its
+ * linears: an 8-bit cache of keys and values, attention over it, its eviction,
+ * and log probabilities (at the end of this file).
  *
  * Conventions
  *   W is m x n: m output features (rows), n input features (columns), y = W x
@@ -51,7 +53,8 @@ extern "C" {
 typedef enum {
     SPQT_OK = 0,
     SPQT_ERR_INVALID_ARG = 1, /* null pointer, non-positive size, ldw < n; a bad index list (checked mode) */
-    SPQT_ERR_UNSUPPORTED = 2, /* bits not in {3,4}, group not in {64,128}, m % group != 0, n too large     */
+    SPQT_ERR_UNSUPPORTED = 2, /* bits not in {3,4}, group not in {64,128}, m % group != 0, n too large;
+                                 a head size, block size or number of heads outside what is documented     */
     SPQT_ERR_ALIGNMENT = 3,   /* a pointer is not aligned as documented                                    */
     SPQT_ERR_WORKSPACE = 4,   /* workspace smaller than spqt_packed_sizes reports                          */
     SPQT_ERR_CUDA = 5,        /* the CUDA runtime reported an error (launch, copy, query)                  */
@@ -508,9 +511,13 @@ spqt_status spqt_probe_arith(int chunks_per_warp, float* sink, size_t sink_float
  *
  * The kernels check what they read of `table` and `length`.  A length that is negative or exceeds the table's row counts as an
  * empty stream; a block number outside the pool is not followed, and what it stands for is not-a-number.  Either sets the status
- * word of the workspace to 3 (spqt_kv_status).  Two entries of the table that name one block are not detected.
+ * word of the workspace to 3 (spqt_kv_status).  Two entries of the table that name one block are not detected: full blocks may be
+ * shared (a common prefix) as long as nothing is accumulated into them; a block that tokens go to, or whose weights count, may not.
  *
  * Positions are the caller's: keys and queries come as they are to be multiplied (rotated, for instance).
+ *
+ * All pointers are of the current device.  The calls read and write the cache in the order of their stream; calls on other streams
+ * have to be ordered by the caller, and need a workspace of their own where they may overlap (so do two graphs that may).
  */
 enum { SPQT_KV_INT8 = 0, SPQT_KV_E4M3 = 1 };
 

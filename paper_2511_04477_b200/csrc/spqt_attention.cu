@@ -64,9 +64,12 @@ template <int D, int ROWS>
 struct AttnShape {
     static constexpr int kWarps = D == 256 ? 4 : 8;
     static constexpr int kTileBytes = 2 * kTile * D;
-    static constexpr int kStages = D <= 96 ? 4 : D == 128 ? 2 : ROWS == 16 ? 2 : 3;
+    static constexpr int kStages = D == 64 ? 4 : D == 96 ? 3 : D == 128 ? 2 : ROWS == 16 ? 2 : 3;
     static constexpr int kCols = ROWS == 16 ? 2 : 1;             // sets of eight columns
     static constexpr int kStride = D + 4;                        // of a row of sums in shared memory: 8 bytes a lane without conflicts
+    static constexpr int kDynamic = kWarps * kStages * kTileBytes + kMaxAttnCtas * ROWS * 8;
+    static constexpr int kStatic = kLengthCache * 4 + kWarps * kStages * 16 + kWarps * ROWS * 8 + kWarps / 2 * ROWS * kStride * 4 + 512;
+    static_assert(kStatic <= 48 * 1024 && kDynamic + kStatic + 1024 <= 227 * 1024, "shared memory of a CTA");
 };
 
 // Tokens of a stream's full blocks, and its tiles: those by 32 tokens, then the open block's by 16.
@@ -865,7 +868,7 @@ template <int FMT, int D, int ROWS>
 cudaError_t launch_attention(const AttnArgs& a, cudaStream_t s)
 {
     using S = AttnShape<D, ROWS>;
-    constexpr size_t smem = (size_t)S::kWarps * S::kStages * S::kTileBytes + (size_t)kMaxAttnCtas * ROWS * sizeof(float2);
+    constexpr size_t smem = S::kDynamic;
     static thread_local int allowed_dev = -1;
     int dev = 0;
     cudaError_t err = cudaGetDevice(&dev);

@@ -46,6 +46,14 @@ def test_head_layouts_and_queries(kv_heads, group, queries, accumulate):
     compare(st, st.queries(kv_heads * group, queries, seed=2, amplitude=1.5), accumulate)
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("group", [4, 8, 16])
+def test_every_head_size_with_few_and_many_rows(fmt, dim, group):
+    st = Streams([0, 33, 700], 2, dim, 32, fmt, seed=dim + group)
+    compare(st, st.queries(2 * group, 1, seed=6), accumulate=True)
+
+
 @pytest.mark.parametrize("fmt,dim,bt,group,queries", [("int8", 128, 32, 4, 1), ("e4m3", 128, 64, 8, 1), ("int8", 64, 16, 5, 2), ("int8", 256, 32, 16, 1), ("e4m3", 96, 128, 1, 1)])
 def test_streams_that_many_ctas_share(fmt, dim, bt, group, queries):
     st = Streams([20011, 7, 4097], 2, dim, bt, fmt, seed=5)
