@@ -121,21 +121,51 @@ struct Vec {
         if constexpr (sizeof(T) == 4) return fadd2(pack2(__uint_as_float(word(2 * i)), __uint_as_float(word(2 * i + 1))), pack2(-base, -base));
         else return less_base(word(i), base, T());
     }
-    __device__ __forceinline__ float top() const               // the largest, not-a-number left out
+    // the larger of two words' values each, not-a-number left out, and the largest of a word
+    static __device__ __forceinline__ unsigned larger(unsigned a, unsigned b)
     {
         if constexpr (sizeof(T) == 4) {
-            return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+            return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
         } else if constexpr (std::is_same<T, __half>::value) {
-            const __half2* h = reinterpret_cast<const __half2*>(&w);
-            const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-            return fmaxf(f.x, f.y);
+            const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+            return *reinterpret_cast<const unsigned*>(&m);
         } else {
-            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
-            const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-            return fmaxf(f.x, f.y);
+            const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+            return *reinterpret_cast<const unsigned*>(&m);
         }
     }
+    static __device__ __forceinline__ float largest_of(unsigned a)
+    {
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(a);
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&a));
+            return fmaxf(f.x, f.y);
+        } else {
+            return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+        }
+    }
+    __device__ __forceinline__ unsigned larger() const { return larger(larger(w.x, w.y), larger(w.z, w.w)); }
+    __device__ __forceinline__ float top() const { return largest_of(larger()); }
 };
+
+// Sum of e^d d, d = x - base, of 16 bytes of values, -infinity adding nothing.  (A call, since the values in earnest seldom need it.)
+template <class T>
+__device__ __noinline__ float without_infinities(uint4 w, float base)
+{
+    const Vec<T> v(w);
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < Vec<T>::P; ++i) {
+        float lo, hi;
+        v.pair(i, lo, hi);
+        t = fmaf(exp_of(lo - base), fmaxf(lo - base, -1e30f), t);
+        t = fmaf(exp_of(hi - base), fmaxf(hi - base, -1e30f), t);
+    }
+    return t;
+}
+
+constexpr int kSlots = 8;
 
 // What a team of threads (a warp, or a CTA) shares.  Two of what the first warp may still read, or set, when the others are at the
 // next row.
@@ -147,7 +177,8 @@ struct LogShared {
     Sums sums[2][NW];
     int listed[2], reached[2], votes;
     float odd[16];                                      // values in front of the first whole 16 bytes and behind the last
-    unsigned short who[32 * NW];                        // threads whose largest reaches the bound
+    float tops[kSlots][32 * NW];                        // the largest of a thread's vectors, those of a few rounds in a slot
+    unsigned short who[kSlots * 32 * NW];               // slots (times the threads) and threads whose largest reaches the bound
 };
 struct LogClusterShared {                               // (in the first CTA's memory)
     Sums parts[kMaxLogCtas];
@@ -173,7 +204,7 @@ struct LogPart {
     __device__ __forceinline__ const void* vec(int i) const { return row + head + (size_t)i * V; }
 };
 
-constexpr int kVecs = 4;                // vectors of a thread on their way at a time
+constexpr int kVecs = 4;                // vectors of a thread on their way at a time: a round
 
 // TEAM threads for a part: 32 or 128 (several teams in the CTA) or the whole CTA.
 template <class T, int TEAM, int LIST>
@@ -185,6 +216,8 @@ struct LogTeam {
     int turn;                           // 0, 1, 0, ... row after row
     Sums sum;
     float largest;                      // (not-a-number is not seen here: some value reaches it; and it makes the sums not-a-number)
+    int slot_shift;                     // log2 of the rounds of a slot
+    float slot_top;
 
     static __device__ __forceinline__ void sync()
     {
@@ -209,7 +242,9 @@ struct LogTeam {
     __device__ __forceinline__ void begin(const LogPart<T>& p)
     {
         sum = {-INFINITY, 0.0f, 0.0f};
-        largest = -INFINITY;
+        largest = slot_top = -INFINITY;
+        const int rounds = (p.vecs + TEAM * kVecs - 1) / (TEAM * kVecs);
+        slot_shift = rounds <= kSlots ? 0 : 32 - __clz((rounds - 1) / kSlots);
         if (tid < p.odd) {
             const float x = (float)p.row[p.place_of_odd(tid)];
             sh.odd[tid] = x;
@@ -219,19 +254,38 @@ struct LogTeam {
         }
         if (tid == 0) sh.listed[turn] = sh.reached[turn] = 0;
     }
-    __device__ __forceinline__ void add(const uint4* w, const LogPart<T>& p, int i0)
+    // a round's vectors, the first at i0 (of all threads at `round` * TEAM * kVecs)
+    __device__ __forceinline__ void add(const uint4* w, const LogPart<T>& p, int i0, int round)
+    {
+        if ((round + 1) * (TEAM * kVecs) <= p.vecs) add_some<true>(w, p, i0);
+        else add_some<false>(w, p, i0);
+        if (a.top > 0 && (((round + 1) & ((1 << slot_shift) - 1)) == 0 || (round + 1) * (TEAM * kVecs) >= p.vecs)) {
+            sh.tops[round >> slot_shift][tid] = slot_top;
+            slot_top = -INFINITY;
+        }
+    }
+    template <bool ALL>
+    __device__ __forceinline__ void add_some(const uint4* w, const LogPart<T>& p, int i0)
     {
         const bool entropy = a.entropy != nullptr;
         float top = -INFINITY;
+        if (ALL) {
+            unsigned m = Vec<T>(w[0]).larger();
 #pragma unroll
-        for (int u = 0; u < kVecs; ++u)
-            if (i0 + u * TEAM < p.vecs) top = fmaxf(top, Vec<T>(w[u]).top());
+            for (int u = 1; u < kVecs; ++u) m = Vec<T>::larger(m, Vec<T>(w[u]).larger());
+            top = fmaxf(top, Vec<T>::largest_of(m));
+        } else {
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u)
+                if (i0 + u * TEAM < p.vecs) top = fmaxf(top, Vec<T>(w[u]).top());
+        }
+        slot_top = fmaxf(slot_top, top);
         const float base = reach(top);
         unsigned long long s = 0ull, t = 0ull;
         float lo, hi;
 #pragma unroll
         for (int u = 0; u < kVecs; ++u)
-            if (i0 + u * TEAM < p.vecs) {
+            if (ALL || i0 + u * TEAM < p.vecs) {
                 const Vec<T> v(w[u]);
 #pragma unroll
                 for (int i = 0; i < Vec<T>::P; ++i) {
@@ -239,7 +293,7 @@ struct LogTeam {
                     unpack2(fmul2(d, pack2(kLog2e, kLog2e)), lo, hi);
                     const unsigned long long e = pack2(exp2_of(lo), exp2_of(hi));
                     s = fadd2(s, e);
-                    if (entropy) ffma2(t, e, d);
+                    if (entropy) t = fma2(e, d, t);
                 }
             }
         unpack2(s, lo, hi);
@@ -250,15 +304,7 @@ struct LogTeam {
             both = 0.0f;
 #pragma unroll
             for (int u = 0; u < kVecs; ++u)
-                if (i0 + u * TEAM < p.vecs) {
-                    const Vec<T> v(w[u]);
-#pragma unroll
-                    for (int i = 0; i < Vec<T>::P; ++i) {
-                        v.pair(i, lo, hi);
-                        both = fmaf(exp_of(lo - base), fmaxf(lo - base, -1e30f), both);
-                        both = fmaf(exp_of(hi - base), fmaxf(hi - base, -1e30f), both);
-                    }
-                }
+                if (ALL || i0 + u * TEAM < p.vecs) both += without_infinities<T>(w[u], base);
         }
         sum.t += both;
     }
@@ -317,24 +363,30 @@ struct LogTeam {
             }
         }
         const float floor = least == 0u ? -INFINITY : value_of(least);
-        // the threads whose largest reaches the bound, or who have met not-a-number; their vectors, by all threads
-        if (value_bits(largest) >= least || sum.s != sum.s) sh.who[atomicAdd(&sh.reached[turn], 1)] = (unsigned short)tid;
+        const int rounds = (p.vecs + TEAM * kVecs - 1) / (TEAM * kVecs);
+        // the slots whose largest reaches the bound, or of threads who have met not-a-number; their vectors, by all threads
+        const bool strange = sum.s != sum.s;
+        if (value_bits(largest) >= least || strange)
+            for (int k = 0; k << slot_shift < rounds; ++k)
+                if (strange || sh.tops[k][tid] >= floor) sh.who[atomicAdd(&sh.reached[turn], 1)] = (unsigned short)(k * TEAM + tid);
         sync();
-        const int shift = 32 - __clz(max(p.vecs - 1, 0) / TEAM), pairs = sh.reached[turn] << shift;   // (2^shift: vectors of a thread, or more)
+        const int shift = slot_shift + 2, pairs = sh.reached[turn] << shift;
+        static_assert(kVecs == 4, "vectors of a round: two bits");
         for (int x = tid; x < pairs; x += TEAM) {
-            const int i = sh.who[x >> shift] + (x & ((1 << shift) - 1)) * TEAM;
+            const int k = sh.who[x >> shift], v = x & ((1 << shift) - 1);
+            const int i = ((k / TEAM << slot_shift) + (v >> 2)) * (TEAM * kVecs) + (v & 3) * TEAM + k % TEAM;
             if (i >= p.vecs) continue;
-            const Vec<T> v(ld_global_v4(p.vec(i)));
+            const Vec<T> w(ld_global_v4(p.vec(i)));
             float lo, hi, any = 0.0f;
 #pragma unroll
             for (int e = 0; e < Vec<T>::P; ++e) {
-                v.pair(e, lo, hi);
+                w.pair(e, lo, hi);
                 any += lo + hi;                                 // (not-a-number if one of them is)
             }
-            if (v.top() >= floor || any != any) {
+            if (w.top() >= floor || any != any) {
 #pragma unroll
                 for (int e = 0; e < Vec<T>::P; ++e) {
-                    v.pair(e, lo, hi);
+                    w.pair(e, lo, hi);
                     if (!(lo < floor)) put(key_of(lo, p.head + i * V + 2 * e));
                     if (!(hi < floor)) put(key_of(hi, p.head + i * V + 2 * e + 1));
                 }
@@ -422,7 +474,7 @@ __global__ void __launch_bounds__(256, 4) token_logprobs_rows_kernel(const LogAr
     constexpr int kTeams = 256 / TEAM, kList = TEAM == 32 ? 256 : TEAM == 128 ? 1024 : kLogList;
     __shared__ LogShared<TEAM / 32, kList> shared[kTeams];
     const int which = threadIdx.x / TEAM, tid = threadIdx.x % TEAM;
-    LogTeam<T, TEAM, kList> team = {shared[which], a, tid, (int)threadIdx.x & 31, tid >> 5, 0, {}, 0.0f};
+    LogTeam<T, TEAM, kList> team = {shared[which], a, tid, (int)threadIdx.x & 31, tid >> 5, 0, {}, 0.0f, 0, 0.0f};
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const T* const logits = static_cast<const T*>(a.logits);
@@ -440,7 +492,7 @@ __global__ void __launch_bounds__(256, 4) token_logprobs_rows_kernel(const LogAr
             uint4 next[kVecs];
             if (i0 + TEAM * kVecs < part.vecs) team.load(next, part, i0 + TEAM * kVecs + tid);
             else if (r + step < rows) team.load(next, LogPart<T>(logits + (long long)(r + step) * a.row_stride, a.vocab), tid);
-            team.add(w, part, i0 + tid);
+            team.add(w, part, i0 + tid, i0 / (TEAM * kVecs));
 #pragma unroll
             for (int u = 0; u < kVecs; ++u) w[u] = next[u];
         }
@@ -463,7 +515,7 @@ __global__ void __launch_bounds__(kPartThreads, 2) token_logprobs_parts_kernel(c
     __shared__ LogShared<kPartThreads / 32, kLogList> shared;
     __shared__ LogClusterShared meet;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    LogTeam<T, kPartThreads, kLogList> team = {shared, a, tid, lane, warp, 0, {}, 0.0f};
+    LogTeam<T, kPartThreads, kLogList> team = {shared, a, tid, lane, warp, 0, {}, 0.0f, 0, 0.0f};
     const int ctas = (int)gridDim.x, rank = (int)blockIdx.x, r = (int)blockIdx.y;
     const int first = rank * a.part, n = max(0, min(a.part, a.vocab - first));
     cluster_arrive();
@@ -476,7 +528,7 @@ __global__ void __launch_bounds__(kPartThreads, 2) token_logprobs_parts_kernel(c
     team.load(w, part, tid);
     team.begin(part);
     for (int i0 = 0; i0 < part.vecs;) {
-        team.add(w, part, i0 + tid);
+        team.add(w, part, i0 + tid, i0 / (kPartThreads * kVecs));
         i0 += kPartThreads * kVecs;
         if (i0 < part.vecs) team.load(w, part, i0 + tid);
     }
