@@ -79,9 +79,14 @@ __device__ __forceinline__ int tiles_of(int n, int shift) { return code_tiles(n,
 
 __device__ __forceinline__ int places_of(int tiles) { return tiles == 0 ? 0 : kRoom + tiles; }
 
-// CTAs that work: not more than leave a tile for every warp.  A CTA's places begin at total * i / ctas.  (In fp64: the products
-// are exact, and a quotient that is no whole number is 1/ctas or more from one.)
-__device__ __forceinline__ int working_ctas(int total, int warps, int most) { return min(max((total + warps - 1) / warps, 1), most); }
+// CTAs that work: one for each segment (`busy` have tiles) where these are so short that to add parts would take longer than to
+// have all the tiles (eight streams of 512 tokens 7.5 us with one, 8.1 with two; of 768 9.0 and 8.2), else not more than leave a tile for every warp.  A CTA's places
+// begin at total * i / ctas.  (In fp64: the products are exact, and a quotient that is no whole number is 1/ctas or more from one.)
+constexpr int kWhole = 20;
+__device__ __forceinline__ int working_ctas(int total, int busy, int warps, int most)
+{
+    return min(max(total <= (kRoom + kWhole) * busy ? busy : (total + warps - 1) / warps, 1), most);
+}
 __device__ __forceinline__ int begin_of(int cta, int total, int ctas) { return (int)((double)total * cta / ctas); }
 __device__ __forceinline__ int owner_of(int place, int total, int ctas) { return (int)(((double)(place + 1LL) * ctas - 1.0) / total); }
 
@@ -158,7 +163,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
     constexpr int NW = S::kWarps, STAGES = S::kStages, NC = S::kCols, CH = D / 16;
     extern __shared__ __align__(128) unsigned char s_ring[];                 // [NW][STAGES][kTileBytes], then s_part
     __shared__ int s_len[kLengthCache];
-    __shared__ int s_scan[NW], s_start[2];
+    __shared__ int s_scan[NW], s_busy[NW], s_start[2];
     __shared__ __align__(16) float s_scale[NW][STAGES][4];                   // k scale of the halves, v scale of the halves
     __shared__ float2 s_ml[NW][ROWS];
     __shared__ __align__(16) float s_o[NW / 2][ROWS][S::kStride];
@@ -172,13 +177,14 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
 
     // ---- which tiles are this CTA's
     const int per = (streams + NW * 32 - 1) / (NW * 32);
-    int mine = 0;
+    int mine = 0, busy = 0;
     for (int i = 0; i < per; ++i) {
         const int st = tid * per + i;
         if (st < streams) {
             const int n = length_or_none((int)ld_global_u32(c.length + st), c, a.status);
             if (st < kLengthCache) s_len[st] = n;
             mine += places_of(tiles_of(n, shift)) * a.row_groups;
+            busy += n > 0;
         }
     }
     int incl = mine;
@@ -187,16 +193,19 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         const int v = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += v;
     }
-    if (lane == 31) s_scan[warp] = incl;
+    busy = __reduce_add_sync(0xffffffffu, busy);
+    if (lane == 31) s_scan[warp] = incl, s_busy[warp] = busy;
     __syncthreads();
     int base = incl - mine, total = 0;
+    busy = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         base += w < warp ? s_scan[w] : 0;
         total += s_scan[w];
+        busy += s_busy[w];
     }
     auto length_of = [&](int st) { return st < kLengthCache ? s_len[st] : length_or_none((int)ld_global_u32(c.length + st), c, a.status); };
-    const int ctas = working_ctas(total, NW, gridDim.x), cta = blockIdx.x;
+    const int ctas = working_ctas(total, busy * a.row_groups, NW, gridDim.x), cta = blockIdx.x;
     if (a.accumulate && cta == 0) {           // for the second kernel
         if (tid == 0) a.begin[streams * a.row_groups] = total;
         for (int st = tid * per, at = base; st < min(streams, (tid + 1) * per); ++st) {
@@ -738,6 +747,14 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                                 if (first + u * kSplit <= c1) add(first + u * kSplit, ahead[u]);
                             k += kAhead * kSplit;
                         }
+#pragma unroll 1
+                        for (; ROWS <= 8 && k + 7 * kSplit <= c1; k += 8 * kSplit) {   // (sixteen rows have no registers left)
+                            float4 y[8];
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) y[u] = sums_of(i, k + u * kSplit);
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) add(k + u * kSplit, y[u]);
+                        }
 #pragma unroll 4
                         for (; k <= c1; k += kSplit) add(k, sums_of(i, k));
                         if (kSplit == 1) {
@@ -779,7 +796,7 @@ constexpr int kNoteWarps = 8;
 template <int ROWS>
 __global__ void __launch_bounds__(kNoteWarps * 32) kv_weights_kernel(const AttnArgs a, int segments)
 {
-    constexpr int N = 16 / ROWS < 2 ? 2 : 16 / ROWS, Q = ROWS / 4;   // places at a time, four rows each
+    constexpr int N = ROWS == 16 ? 2 : 4, Q = ROWS / 4;   // places at a time, four rows each
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, shift = a.shift;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -801,30 +818,38 @@ __global__ void __launch_bounds__(kNoteWarps * 32) kv_weights_kernel(const AttnA
         for (int u = 0; u < N; ++u) old[u] = seg[u] >= 0 ? *to[u] : 0.0f;
         for (int rg = 0; rg < a.row_groups; ++rg) {
             const int rows = min(ROWS, a.rows - rg * ROWS);
-            float4 s[N][Q], l[N][2 * Q];
+            float4 s[N][Q];
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int sg = max(seg[u], 0), x = rg == 0 ? x0 + u : x0 + u - a.begin[sg] + a.begin[sg + rg];
                 const float4* const from = reinterpret_cast<const float4*>(a.scores + ((size_t)(seg[u] < 0 ? 0 : x) * kTile + lane) * ROWS);
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (seg[u] >= 0 && 4 * q < rows) s[u][q] = from[q];
+            }
+            // (the sums of a segment's rows: those of the place before them in most cases)
+            float4 l[2 * Q];
+            auto load_sums = [&](int sg) {
                 const float4* const lse = reinterpret_cast<const float4*>(a.lse + (size_t)(sg + rg) * ROWS);
 #pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    if (seg[u] < 0 || 4 * q >= rows) continue;
-                    s[u][q] = from[q];
-                    l[u][2 * q] = lse[2 * q], l[u][2 * q + 1] = lse[2 * q + 1];
-                }
-            }
+                for (int q = 0; q < 2 * Q; ++q) l[q] = lse[q];
+            };
+            int have = max(seg[N - 1], 0);
+            load_sums(have);
 #pragma unroll
-            for (int u = 0; u < N; ++u)
+            for (int u = 0; u < N; ++u) {
+                if (seg[u] < 0) continue;
+                if (seg[u] != have) load_sums(have = seg[u]);
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {
-                    if (seg[u] < 0 || 4 * q >= rows) continue;
-                    const float4 e = s[u][q], l0 = l[u][2 * q], l1 = l[u][2 * q + 1];
+                    if (4 * q >= rows) continue;
+                    const float4 e = s[u][q], l0 = l[2 * q], l1 = l[2 * q + 1];
                     sum[u] = fmaf(exp2_fast(e.x - l0.x), l0.y, sum[u]);
                     if (4 * q + 1 < rows) sum[u] = fmaf(exp2_fast(e.y - l0.z), l0.w, sum[u]);
                     if (4 * q + 2 < rows) sum[u] = fmaf(exp2_fast(e.z - l1.x), l1.y, sum[u]);
                     if (4 * q + 3 < rows) sum[u] = fmaf(exp2_fast(e.w - l1.z), l1.w, sum[u]);
                 }
+            }
         }
 #pragma unroll
         for (int u = 0; u < N; ++u)
@@ -834,7 +859,9 @@ __global__ void __launch_bounds__(kNoteWarps * 32) kv_weights_kernel(const AttnA
 
 // ---------------------------------------------------------------- host
 
-inline int rows_of(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+// Rows that go through the product together.  Few streams are cut into many parts, whose sums one CTA adds: sixteen rows of one
+// stream of 65536 tokens by eight 20.0 us, by sixteen 45.1; of sixteen streams of 8192 19.3 and 19.8, of 32 31.1 and 26.5.
+inline int rows_of(int rows, long long streams) { return rows <= 4 ? 4 : rows <= 8 || streams <= 16 ? 8 : 16; }
 
 struct AttnWorkspace {
     size_t arrived, begin, ml, o, lse, tiles, scores, bytes;   // (what stays zero between calls at a place that depends on nothing)
@@ -843,8 +870,9 @@ struct AttnWorkspace {
 // false where the tiles' numbers would pass 31 bits
 inline bool attention_workspace(const spqt_kv_cache& c, int group, int queries, AttnWorkspace* w)
 {
-    const int rows = group * queries, R = rows_of(rows), groups = (rows + R - 1) / R;
-    const long long streams = (long long)c.batch * c.kv_heads, segments = streams * groups;
+    const long long streams = (long long)c.batch * c.kv_heads;
+    const int rows = group * queries, R = rows_of(rows, streams), groups = (rows + R - 1) / R;
+    const long long segments = streams * groups;
     const long long tiles = segments * (((long long)c.table_width * c.block_tokens + kTile - 1) / kTile + 8 + kRoom);
     if (segments > kMaxStreams || tiles > 0x7fffffffLL) return false;
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
@@ -889,7 +917,7 @@ cudaError_t launch_attention(const AttnArgs& a, cudaStream_t s)
 template <int FMT, int D>
 cudaError_t launch_rows(const AttnArgs& a, cudaStream_t s)
 {
-    const int r = rows_of(a.rows);
+    const int r = rows_of(a.rows, (long long)a.c.batch * a.c.kv_heads);
     return r == 4 ? launch_attention<FMT, D, 4>(a, s) : r == 8 ? launch_attention<FMT, D, 8>(a, s) : launch_attention<FMT, D, 16>(a, s);
 }
 
@@ -947,7 +975,7 @@ spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long lo
     st = check_kv_workspace(workspace, workspace_bytes, accumulate ? w.bytes : w.lse);
     if (st != SPQT_OK) return st;
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
-    const int group = q_heads / cache->kv_heads, rows = group * queries, R = rows_of(rows);
+    const int group = q_heads / cache->kv_heads, rows = group * queries, R = rows_of(rows, (long long)cache->batch * cache->kv_heads);
     const AttnArgs a = {*cache, static_cast<const __half*>(q), q_batch_stride, q_token_stride, static_cast<__half*>(out), out_batch_stride, out_token_stride,
                         group, queries, rows, (rows + R - 1) / R, 31 - __builtin_clz((unsigned)cache->block_tokens), accumulate ? 1 : 0, scale * 1.4426950408889634f, static_cast<int*>(status_word(workspace)),
                         reinterpret_cast<int*>(ws + w.begin), reinterpret_cast<int*>(ws + w.arrived), reinterpret_cast<float2*>(ws + w.ml),
