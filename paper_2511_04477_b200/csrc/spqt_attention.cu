@@ -794,9 +794,11 @@ constexpr int kNoteWarps = 8;
 // The probabilities that a tile's tokens have received, a lane per token and a warp for a few places at a time: their notes, then
 // scores, sums and weights are on their way together.
 template <int ROWS>
-__global__ void __launch_bounds__(kNoteWarps * 32) kv_weights_kernel(const AttnArgs a, int segments)
+__global__ void __launch_bounds__(kNoteWarps * 32, ROWS == 16 ? 2 : 4) kv_weights_kernel(const AttnArgs a, int segments)
 {
-    constexpr int N = ROWS == 16 ? 2 : 4, Q = ROWS / 4;   // places at a time, four rows each
+    // places at a time, four rows each.  (Eight sequences of 8192 tokens, eight rows: two at a time on four CTAs an SM 43.4 us with the
+    // attention, four on two 44.6; four rows 41.5 and 42.3; sixteen rows spill with four CTAs, 38.5 against 35.2)
+    constexpr int N = 2, Q = ROWS / 4;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, shift = a.shift;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
