@@ -517,7 +517,10 @@ spqt_status spqt_probe_arith(int chunks_per_warp, float* sink, size_t sink_float
  * Positions are the caller's: keys and queries come as they are to be multiplied (rotated, for instance).
  *
  * All pointers are of the current device.  The calls read and write the cache in the order of their stream; calls on other streams
- * have to be ordered by the caller, and need a workspace of their own where they may overlap (so do two graphs that may).
+ * have to be ordered by the caller, and need a workspace of their own where they may overlap (so do two graphs that may).  The
+ * workspace of these calls is not one of the products': each finds its own part of it zero.
+ *
+ * Codes are what spqt_kv_append writes; e4m3 codes of the caller's own must not be not-a-number (a scale may).
  */
 enum { SPQT_KV_INT8 = 0, SPQT_KV_E4M3 = 1 };
 
@@ -569,6 +572,7 @@ spqt_status spqt_kv_workspace(const spqt_kv_cache* cache, int q_heads, int queri
  * head (one call adds to each weight once, so that the sums do not depend on an order).  Sums and the softmax are held in fp32, p
  * enters the product to 2^-22 of the largest.  At most 64 query heads per kv head.
  *   workspace : spqt_kv_workspace bytes, 16-byte aligned, zeroed once by the caller.  Calls that may overlap need two.
+ *   out must not overlap q or the cache.
  */
 spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long long q_batch_stride, long long q_token_stride, int q_heads,
                               int queries, float scale, int accumulate, void* out, long long out_batch_stride,

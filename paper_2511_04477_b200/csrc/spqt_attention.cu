@@ -225,8 +225,9 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
     if (total == 0 || cta >= ctas) return;
     const int t0 = begin_of(cta, total, ctas), t1 = begin_of(cta + 1, total, ctas);
     if (t0 >= base && t0 < base + mine) {
+        // (bounded here and below, should lengths change while the kernel runs)
         int st = tid * per, at = base;
-        for (;; ++st) {
+        for (; st + 1 < streams; ++st) {
             const int k = places_of(tiles_of(length_of(st), shift)) * a.row_groups;
             if (t0 < at + k) break;
             at += k;
@@ -235,7 +236,10 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         s_start[1] = at;
     }
     __syncthreads();
-    const int stream0 = s_start[0], n0 = length_of(stream0), tiles0 = tiles_of(n0, shift), rg0 = (t0 - s_start[1]) / places_of(tiles0);
+    const int segments = streams * a.row_groups;
+    const int stream0 = s_start[0], n0 = length_of(stream0), tiles0 = tiles_of(n0, shift);
+    if (tiles0 == 0) return;
+    const int rg0 = min((t0 - s_start[1]) / places_of(tiles0), a.row_groups - 1);
     const int seg0 = stream0 * a.row_groups + rg0, begin0 = s_start[1] + rg0 * places_of(tiles0) + kRoom;
 
     // ---- the tiles ahead: a walk over this warp's tiles that knows the segment of each; first the block numbers, one tile later
@@ -248,7 +252,10 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
                 w_tile = kNoTile;
                 return;
             }
-            ++w_seg;
+            if (++w_seg >= segments) {
+                w_tile = kNoTile;
+                return;
+            }
             w_n = length_of(w_seg / a.row_groups);
             const int k = tiles_of(w_n, shift);
             if (k == 0) continue;
@@ -603,10 +610,9 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
         const int this_seg = seg, this_begin = begin;
         begin = end;
         do {
-            ++seg;
-            n = begin + kRoom < t1 ? length_of(seg / a.row_groups) : 1;
+            n = ++seg < segments && begin + kRoom < t1 ? length_of(seg / a.row_groups) : 1;
         } while (n == 0);
-        begin += kRoom;
+        begin = seg < segments ? begin + kRoom : t1;
         if (begin < t1) load_queries();
 
         // ---- the warps' sums: to the CTA's largest M, then by way of shared memory, half the warps at a time

@@ -583,7 +583,7 @@ spqt_status spqt_kv_evict(const spqt_kv_cache* cache, int keep, int first, int r
     static thread_local int allowed_dev = -1;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return launched(cudaErrorInvalidDevice);
-    if (smem > 48 * 1024 && allowed_dev != dev) {
+    if (smem > 40 * 1024 && allowed_dev != dev) {   // (48 KB with the kernel's own need no leave)
         const cudaError_t err = cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxTableWidth * 8);
         if (err != cudaSuccess) return launched(err);
         allowed_dev = dev;

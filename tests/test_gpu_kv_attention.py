@@ -60,6 +60,76 @@ def test_streams_that_many_ctas_share(fmt, dim, bt, group, queries):
     compare(st, st.queries(2 * group, queries, seed=3, amplitude=3.0), accumulate=True)
 
 
+@pytest.mark.parametrize("fmt,dim,bt", [("int8", 128, 32), ("e4m3", 64, 16), ("int8", 96, 64), ("e4m3", 256, 128), ("e4m3", 128, 64), ("int8", 256, 16)])
+@pytest.mark.parametrize("group,queries", [(16, 1), (3, 4), (8, 3), (5, 7)])
+def test_many_rows_of_many_streams(fmt, dim, bt, group, queries):
+    """More than sixteen streams: sixteen rows at a time, in one group or in several."""
+    lengths = [0, 1, 2, 16, 17, 40, 130, 333, 500, 1025]
+    st = Streams(lengths, 2, dim, bt, fmt, seed=group + queries)
+    compare(st, st.queries(2 * group, queries, seed=7, amplitude=1.5), accumulate=True)
+
+
+def test_offsets_beyond_32_bits():
+    """The last blocks of a pool whose codes take more than 2^32 bytes, against the same contents in a small pool."""
+    st = Streams([300], 1, 256, 128, "int8", seed=31)
+    q = torch.from_numpy(st.queries(4, 1, seed=32)).cuda()
+    small = spqt.spqt_kv_attention(st.cache, q, st.workspace(4), accumulate=True)
+    c, far = st.cache, (1 << 32) // (128 * 256) + 64
+    big = far + c.k_codes.shape[0]
+    codes = [torch.empty((big, 128, 256), dtype=torch.int8, device="cuda") for _ in range(2)]
+    scales = [torch.full((big,), float("nan"), device="cuda") for _ in range(2)]
+    weight = torch.zeros((big, 128), device="cuda")
+    for to, of in zip(codes + scales, (c.k_codes, c.v_codes, c.k_scale, c.v_scale)):
+        to[far:] = of
+    weight[far:] = torch.from_numpy(st.weight).cuda()
+    table = torch.where(c.table >= 0, c.table + far, c.table)
+    other = spqt.KVCache(*codes, *scales, c.k_tail, c.v_tail, table, c.length, weight)
+    ws = spqt.new_kv_workspace(other, 4)
+    out = spqt.spqt_kv_attention(other, q, ws, accumulate=True)
+    assert torch.equal(out, small) and torch.equal(weight[far:], c.weight) and torch.count_nonzero(weight[:far]) == 0
+    k = [torch.zeros((1, 300, 1, 256), dtype=torch.float16, device="cuda") for _ in range(4)]
+    spqt.spqt_kv_read(c, k[0], k[1], ws)
+    spqt.spqt_kv_read(other, k[2], k[3], ws)
+    assert torch.equal(k[0], k[2]) and torch.equal(k[1], k[3])
+    new = torch.randn((1, 84, 1, 256), device="cuda").half()
+    spqt.spqt_kv_append(other, new, new, ws)                # fills the block at the end of the pool
+    assert spqt.spqt_kv_status(ws) == 0 and other.length.tolist() == [[384]]
+    spqt.spqt_kv_read(other, k[0], k[1], ws)                # (the first 300 tokens)
+    assert bool(((k[0][0, 256:300] - k[2][0, 256:300]).abs() <= k[2][0, 256:300].abs().max() * 2 ** -7 + new.abs().max() * 2 ** -7).all())
+
+
+def test_two_calls_at_once():
+    """On two streams with a workspace each, over one cache."""
+    st = Streams([3000, 70], 2, 128, 32, "int8", seed=33)
+    qs = [torch.from_numpy(st.queries(8, 1, seed=34 + i)).cuda() for i in range(2)]
+    want = [spqt.spqt_kv_attention(st.cache, q, st.workspace(8)) for q in qs]
+    ws = [st.workspace(8) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for i in range(2):
+            outs[i].append(spqt.spqt_kv_attention(st.cache, qs[i], ws[i], stream=streams[i]))
+            outs[i][-1].record_stream(streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in outs[i])
+
+
+def test_a_workspace_for_several_shapes():
+    """One workspace, the largest need, for caches of other shapes in turn; nothing of one call is left for the next."""
+    sts = [Streams([2000, 5], 2, 128, 32, "int8", seed=35), Streams([900], 1, 64, 16, "e4m3", seed=36), Streams([4000] * 3, 3, 96, 64, "int8", seed=37)]
+    ws = torch.zeros(max(st.workspace(16 * st.H, 2).numel() for st in sts), dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        for st, q_heads, queries in zip(sts, (8, 16, 3), (2, 1, 2)):
+            q = st.queries(q_heads, queries, seed=38)
+            st.cache.weight.copy_(torch.from_numpy(st.weight))
+            out = attend(st, q, True, ws=ws)
+            want, tol, got, got_tol = st.attention(q)
+            check(out, want, tol)
+            check(st.cache.weight, st.weight + got, got_tol)
+
+
 def test_more_streams_than_their_lengths_are_kept_of():
     rng = np.random.Generator(np.random.PCG64(9))
     lengths = rng.integers(0, 70, (420, 3)) * (rng.random((420, 3)) < 0.7)      # streams of their own lengths, many empty

@@ -311,7 +311,7 @@ def test_evict(bt, keep, first, recent, in_place):
 
 
 @pytest.mark.parametrize("kind", ["heavy", "equal", "few values", "zeros and signs", "not finite"])
-@pytest.mark.parametrize("width", [1, 600, 4096])
+@pytest.mark.parametrize("width", [1, 600, 1500, 4096])
 def test_evict_of_long_rows_and_equal_weights(kind, width):
     def weight(rng, shape):
         if kind == "heavy":
@@ -331,6 +331,13 @@ def test_evict_of_long_rows_and_equal_weights(kind, width):
     c, w = plain_cache(lengths, 1, bt, width, seed=width, weight=weight)
     for keep, first, recent in ((width // 3, min(1, width // 3), min(width // 3, 2) // 2), (max(1, width - 1), 0, 0)):
         check_evict(c, w, keep, first, recent)
+
+
+@pytest.mark.parametrize("width", [5119, 6143, 6144, 16384])
+def test_evict_of_the_longest_rows(width):
+    """Rows for which a CTA needs more shared memory than it has without asking."""
+    c, w = plain_cache([width * 16, width * 16 - 1], 1, 16, width, seed=width, weight=HEAVY)
+    check_evict(c, w, width // 2 + 1, 2, 3)
 
 
 def test_evict_refuses():
