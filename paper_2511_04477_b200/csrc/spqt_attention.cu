@@ -20,7 +20,8 @@
 // segment with some room in front for what it costs beside its tiles, and cut into equal parts, one per CTA; the warps of a CTA take
 // its tiles in turn, each with a ring of tiles on their way (cp.async, so that a block number is all that is needed ahead).  A segment
 // that lies within one CTA is finished there; of the others the CTA that comes last adds the parts, in the order of the CTAs.  Where
-// weights are accumulated, a second kernel turns the scores that the first one left into probabilities.
+// weights are accumulated, a second kernel turns the scores that the first one left into probabilities.  Few segments of caches that
+// hold little go the other way (by_clusters): a cluster of CTAs each, whose sums meet through its shared memory, weights included.
 #include <cuda_fp8.h>
 
 #include "spqt_common.cuh"

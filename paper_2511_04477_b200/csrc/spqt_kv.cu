@@ -336,7 +336,8 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv_read_kernel(const ReadArgs
 // ---------------------------------------------------------------- eviction
 
 constexpr int kMostEvictWarps = 32;
-constexpr int kOwnKeys = 32;      // keys of a lane, where one warp looks for the bound
+constexpr int kOwnKeys = 16;      // keys of a lane, where one warp or four look for the bound
+constexpr int kBoundWarps = 4;    // (128 threads are the fewest of a CTA)
 
 struct EvictArgs {
     spqt_kv_cache c;
@@ -353,6 +354,29 @@ __device__ __forceinline__ unsigned ordered(float f)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Sums over 2^k neighbouring lanes of N values each: lanes exchange halves of what they still have, then (one value left) add.  A lane's
+// result is of value `which`.
+template <int N, int LANES>
+__device__ __forceinline__ double sums_over(const double* v, int lane, int bit, int* which)
+{
+    if constexpr (LANES == 1) {
+        return v[0];
+    } else if constexpr (N > 1) {
+        const bool upper = (lane & bit) != 0;
+        double w[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const double keep = upper ? v[i + N / 2] : v[i], send = upper ? v[i] : v[i + N / 2];
+            w[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+        }
+        if (upper) *which += N / 2;
+        return sums_over<N / 2, LANES / 2>(w, lane, bit << 1, which);
+    } else {
+        const double w = v[0] + __shfl_xor_sync(0xffffffffu, v[0], bit);
+        return sums_over<1, LANES / 2>(&w, lane, bit << 1, which);
+    }
+}
+
 // How many of the CTA's values are true, and how many are in threads before this one (in thread order).
 __device__ __forceinline__ int count_before(bool v, int* s_warps, int* all)
 {
@@ -366,17 +390,72 @@ __device__ __forceinline__ int count_before(bool v, int* s_warps, int* all)
     return __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0) + __popc(mask & ((1u << lane) - 1u));
 }
 
-// One CTA per stream: the blocks' sums as ordered whole numbers in shared memory beside the row of the table; the m-th largest bit
-// by bit; then one pass in order.  The weights are read once, all loads of a row of up to 32 K tokens in flight together; the rest is
-// a chain of steps.  Up to 1024 keys are one warp's, without a barrier of the CTA for every bit: that takes 0.2 to 0.3 us, by
-// __syncthreads_count as by counts in shared memory (sixteen times 32768 tokens 13.8 and 17.3 us).
+// The m-th largest of `count` keys, by WARPS warps (0: by the whole CTA) which call this together: the keys' bits from the top, two a
+// step, since three counts take hardly longer than one.  `key`: it; `equal`: how many of the keys equal to it are among the m;
+// `exactly`: all are.  A thread keeps up to KEYS keys in registers, or (KEYS 0) reads them anew for each step.
+template <int KEYS, int WARPS>
+__device__ __forceinline__ void find_bound(const unsigned* keys, int count, int m, int4 (*s_count)[kMostEvictWarps], unsigned* key, int* equal, bool* exactly)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int warps = WARPS ? WARPS : blockDim.x >> 5, threads = warps * 32;
+    unsigned k[KEYS ? KEYS : 1];
+    if constexpr (KEYS > 0) {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) k[i] = i * threads + tid < count ? keys[i * threads + tid] : 0u;   // (0 reaches no trial)
+    }
+    const int mine = (count + threads - 1) / threads;
+    int parity = 0;
+    auto reach = [&](unsigned t1, unsigned t2, unsigned t3) {
+        int3 c = make_int3(0, 0, 0);
+        if constexpr (KEYS > 0) {
+#pragma unroll
+            for (int i = 0; i < KEYS; i += 4) {
+                if (i >= mine) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c.x += k[i + e] >= t1, c.y += k[i + e] >= t2, c.z += k[i + e] >= t3;
+            }
+        } else {
+            for (int j = tid; j < count; j += threads) {
+                const unsigned v = keys[j];
+                c.x += v >= t1, c.y += v >= t2, c.z += v >= t3;
+            }
+        }
+        c.x = __reduce_add_sync(0xffffffffu, c.x), c.y = __reduce_add_sync(0xffffffffu, c.y), c.z = __reduce_add_sync(0xffffffffu, c.z);
+        if constexpr (WARPS != 1) {
+            parity ^= 1;                    // (counts of the step before may still be read)
+            if (lane == 0) s_count[parity][warp] = make_int4(c.x, c.y, c.z, 0);
+            if constexpr (WARPS) asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
+            else __syncthreads();
+            const int4 part = lane < warps ? s_count[parity][lane] : make_int4(0, 0, 0, 0);
+            c.x = __reduce_add_sync(0xffffffffu, part.x), c.y = __reduce_add_sync(0xffffffffu, part.y), c.z = __reduce_add_sync(0xffffffffu, part.z);
+        }
+        return c;
+    };
+    *key = 0u, *equal = m, *exactly = false;
+    for (int bit = 30; bit >= 0 && !*exactly; bit -= 2) {
+        const unsigned t1 = *key | 1u << bit, t2 = *key | 2u << bit, t3 = *key | 3u << bit;
+        const int3 c = reach(t1, t2, t3);
+        *key = c.z >= m ? t3 : c.y >= m ? t2 : c.x >= m ? t1 : *key;
+        *exactly = c.z == m || c.y == m || c.x == m;
+    }
+    if (!*exactly && *key != 0xffffffffu) *equal = m - reach(*key + 1u, 0xffffffffu, 0xffffffffu).x;
+}
+
+// One CTA per stream: the blocks' sums as ordered whole numbers in shared memory beside the row of the table; the m-th largest by
+// find_bound; then one pass in order.  The weights are read once, all loads of a row of up to 32 K tokens in flight together; the
+// rest is a chain of steps.  Up to 512 keys are one warp's, up to 2048 four warps', which meet at a barrier of their own: sixteen
+// times 32768 tokens 8.0 us (one warp with 1024 keys 11.5, two with 512 each 8.5, eight with 128 each 8.2; a barrier of the CTA for
+// every bit 13.8), one of 4100 tokens 4.7.
+template <int BT>
 __global__ void __launch_bounds__(1024) kv_evict_kernel(const EvictArgs a)
 {
     extern __shared__ unsigned s_dyn[];     // keys [table_width], then the row of the table [table_width]
     __shared__ int s_warps[kMostEvictWarps], s_found[3];
+    __shared__ int4 s_count[2][kMostEvictWarps];
     const spqt_kv_cache& c = a.c;
     const int stream = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
-    const int bt = c.block_tokens, width = c.table_width, shift = 31 - __clz(bt);
+    constexpr int bt = BT, shift = BT == 16 ? 4 : BT == 32 ? 5 : BT == 64 ? 6 : 7;
+    const int width = c.table_width;
     unsigned* const s_key = s_dyn;
     int* const s_row = reinterpret_cast<int*>(s_dyn + width);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -396,32 +475,31 @@ __global__ void __launch_bounds__(1024) kv_evict_kernel(const EvictArgs a)
         return;
     }
     // sums: bt / 4 lanes a block, four weights a lane, in fp64 (the order of the sum is then of no consequence to the rounded one
-    // but in one case of 2^29)
-    const int lanes = bt >> 2, at_once = 32 / lanes, sub = lane / lanes, l = lane % lanes;
-    constexpr int kU = 8;
-    for (int j0 = warp * at_once * kU; j0 < closed; j0 += (threads >> 5) * at_once * kU) {
-        float4 w[kU];
+    // but in one case of 2^29).  A lane has N blocks, so that the lanes of a block can share the additions.
+    constexpr int kLanes = BT / 4, kAtOnce = 32 / kLanes, N = kLanes < 8 ? kLanes : 8;
+    const int sub = lane / kLanes, l = lane % kLanes, turn = (threads >> 5) * kAtOnce;
+    for (int j0 = warp * kAtOnce; j0 < closed; j0 += turn * N) {       // (short rows: a block or few for every warp)
+        float4 w[N];
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            const int j = j0 + u * at_once + sub;
+        for (int u = 0; u < N; ++u) {
+            const int j = j0 + u * turn + sub;
             const unsigned id = j < closed ? (unsigned)s_row[j] : 0xffffffffu;
             w[u] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (id < (unsigned)c.blocks) w[u] = *reinterpret_cast<const float4*>(c.weight + ((size_t)id << shift) + 4 * l);
         }
-        double v[kU];
+        double v[N];
 #pragma unroll
-        for (int u = 0; u < kU; ++u) v[u] = ((double)w[u].x + w[u].y) + ((double)w[u].z + w[u].w);
-        for (int o = 1; o < lanes; o <<= 1)
-#pragma unroll
-            for (int u = 0; u < kU; ++u) v[u] += __shfl_xor_sync(0xffffffffu, v[u], o);
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            const int j = j0 + u * at_once + sub;
-            if (l == 0 && j < closed) {
-                const bool known = (unsigned)s_row[j] < (unsigned)c.blocks;
-                s_key[j] = known ? ordered((float)v[u]) : 0u;      // (what no block stands behind leaves first)
-                if (!known) refuse(a.status);
-            }
+        for (int u = 0; u < N; ++u) {
+            v[u] = 0.0;
+            if (j0 + u * turn < closed) v[u] = ((double)w[u].x + w[u].y) + ((double)w[u].z + w[u].w);
+        }
+        int u = 0;
+        const double sum = sums_over<N, kLanes>(v, lane, 1, &u);
+        const int j = j0 + u * turn + sub;
+        if (j < closed && l < N) {           // (lanes beyond have the same sums again)
+            const bool known = (unsigned)s_row[j] < (unsigned)c.blocks;
+            s_key[j] = known ? ordered((float)sum) : 0u;               // (what no block stands behind leaves first)
+            if (!known) refuse(a.status);
         }
     }
     __syncthreads();
@@ -430,52 +508,18 @@ __global__ void __launch_bounds__(1024) kv_evict_kernel(const EvictArgs a)
     unsigned key = 0u;                      // its bits so far
     int equal = m;                          // of the keys equal to it only the first so many stay
     bool exactly = false;                   // m keys reach it, so that all that do stay
-    if (m > 0 && hi - lo <= 32 * kOwnKeys) {   // the first warp alone, which keeps the keys in registers
-        if (warp == 0) {
-            const int mine = (hi - lo + 31) / 32;
-            unsigned k[kOwnKeys];
-#pragma unroll
-            for (int i = 0; i < kOwnKeys; ++i) k[i] = lo + i * 32 + lane < hi ? s_key[lo + i * 32 + lane] : 0u;   // (0 reaches no trial)
-            auto reach = [&](unsigned trial) {
-                int v = 0;
-#pragma unroll
-                for (int i = 0; i < kOwnKeys / 4; ++i) v += k[i] >= trial;
-                if (mine > kOwnKeys / 4) {
-#pragma unroll
-                    for (int i = kOwnKeys / 4; i < kOwnKeys; ++i) v += k[i] >= trial;
-                }
-                return __reduce_add_sync(0xffffffffu, v);
-            };
-            for (int bit = 31; bit >= 0 && !exactly; --bit) {
-                const unsigned trial = key | 1u << bit;
-                const int all = reach(trial);
-                if (all >= m) key = trial;
-                exactly = all == m;
-            }
-            if (!exactly && key != 0xffffffffu) equal = m - reach(key + 1u);
-            if (lane == 0) s_found[0] = (int)key, s_found[1] = equal, s_found[2] = exactly;
+    if (m > 0) {
+        const int count = hi - lo;
+        if (count <= 32 * kOwnKeys) {
+            if (warp == 0) find_bound<kOwnKeys, 1>(s_key + lo, count, m, s_count, &key, &equal, &exactly);
+        } else if (count <= 32 * kOwnKeys * kBoundWarps) {
+            if (warp < kBoundWarps) find_bound<kOwnKeys, kBoundWarps>(s_key + lo, count, m, s_count, &key, &equal, &exactly);
+        } else {
+            find_bound<0, 0>(s_key + lo, count, m, s_count, &key, &equal, &exactly);
         }
+        if (tid == 0) s_found[0] = (int)key, s_found[1] = equal, s_found[2] = exactly;
         __syncthreads();
         key = (unsigned)s_found[0], equal = s_found[1], exactly = s_found[2] != 0;
-    } else if (m > 0) {
-        auto reach = [&](unsigned trial) {  // how many keys do, in every thread
-            int v = 0;
-            for (int j = lo + tid; j < hi; j += threads) v += s_key[j] >= trial;
-            v = __reduce_add_sync(0xffffffffu, v);
-            __syncthreads();
-            if (tid == 0) s_found[0] = 0;
-            __syncthreads();
-            if (lane == 0) atomicAdd(&s_found[0], v);
-            __syncthreads();
-            return s_found[0];
-        };
-        for (int bit = 31; bit >= 0 && !exactly; --bit) {
-            const unsigned trial = key | 1u << bit;
-            const int all = reach(trial);
-            if (all >= m) key = trial;
-            exactly = all == m;
-        }
-        if (!exactly && key != 0xffffffffu) equal = m - reach(key + 1u);
     }
     // in order: blocks that stay to the front, the open one, those that leave, the rest where it was
     const int some = n & (bt - 1) ? 1 : 0;
@@ -584,14 +628,17 @@ spqt_status spqt_kv_evict(const spqt_kv_cache* cache, int keep, int first, int r
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return launched(cudaErrorInvalidDevice);
     if (smem > 40 * 1024 && allowed_dev != dev) {   // (48 KB with the kernel's own need no leave)
-        const cudaError_t err = cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxTableWidth * 8);
-        if (err != cudaSuccess) return launched(err);
+        for (auto kernel : {kv_evict_kernel<16>, kv_evict_kernel<32>, kv_evict_kernel<64>, kv_evict_kernel<128>}) {
+            const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxTableWidth * 8);
+            if (err != cudaSuccess) return launched(err);
+        }
         allowed_dev = dev;
     }
     const EvictArgs a = {*cache, keep, first, recent, table_out, length_out, static_cast<int*>(status_word(workspace))};
     // a thread per block of a row, and some more for the loads of short ones
     const int threads = cache->table_width <= 128 ? 128 : cache->table_width <= 512 ? 512 : 1024;
-    return launched(launch_overlapping(kv_evict_kernel, dim3(cache->batch * cache->kv_heads), threads, smem, static_cast<cudaStream_t>(stream), a));
+    const auto kernel = cache->block_tokens == 16 ? kv_evict_kernel<16> : cache->block_tokens == 32 ? kv_evict_kernel<32> : cache->block_tokens == 64 ? kv_evict_kernel<64> : kv_evict_kernel<128>;
+    return launched(launch_overlapping(kernel, dim3(cache->batch * cache->kv_heads), threads, smem, static_cast<cudaStream_t>(stream), a));
 }
 
 spqt_status spqt_kv_status(const void* workspace, int* status_host, void* stream)

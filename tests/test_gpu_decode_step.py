@@ -1,5 +1,9 @@
 """The calls of a decode step one after the other, as a serving loop makes them: linear, append, attention with accumulated weights,
 eviction, linear, head, log probabilities; in a stream and in a replayed graph, against the same steps in 64 bits."""
+import pathlib
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -126,3 +130,51 @@ def test_the_decode_workload_runs():
     r = sweep.run_decode(layers=1, context=512, keep=128, tokens=32)
     assert r["device_status"] == 0 and r["length"] == 128 and r["tokens"] == 32 and r["ms_per_token"] > 0
     assert np.isfinite(r["logprob"]) and 0 <= r["entropy"] <= np.log(sweep.DECODE_VOCAB) and len(set(r["top_index"])) == 5
+
+
+FIRST_CALLS_IN_A_GRAPH = """
+import torch
+from paper_2511_04477_b200 import binding as spqt
+torch.manual_seed(0)
+def caches():
+    torch.manual_seed(1)
+    c = spqt.KVCache.new(2, 2, 128, 16, 64, width, weight=True)
+    c.table.copy_(torch.arange(4 * 16, dtype=torch.int32, device="cuda").view(2, 2, 16).repeat(1, 1, width // 16))
+    for x in (c.k_codes, c.v_codes, c.weight, c.k_tail, c.v_tail):
+        x.zero_()
+    return c
+def step(c, ws, out):
+    spqt.spqt_kv_append(c, *kv, ws)
+    spqt.spqt_kv_attention(c, q, ws, accumulate=True, out=out)
+    spqt.spqt_kv_evict(c, 1, ws)
+    return spqt.spqt_token_logprobs(logits, token, top=3)
+kv = [torch.randn(2, 40, 2, 128, device="cuda").half() for _ in range(2)]
+q = torch.randn(2, 1, 8, 128, device="cuda").half()
+logits, token = torch.randn(2, 500, device="cuda").half(), torch.tensor([3, 7], dtype=torch.int32, device="cuda")
+for width in (16, 2048):
+    runs = []
+    for graph in (True, False):
+        c = caches()
+        ws = spqt.new_kv_workspace(c, 8)
+        out = torch.zeros(2, 1, 8, 128, dtype=torch.float16, device="cuda")
+        torch.cuda.synchronize()
+        if graph:
+            s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                scores = step(c, ws, out)
+            g.replay()
+        else:
+            scores = step(c, ws, out)
+        torch.cuda.synchronize()
+        assert spqt.spqt_kv_status(ws) == 0 and c.length.tolist() == [[24, 24], [24, 24]]
+        runs.append([out, c.table, c.weight, c.k_codes, c.v_tail[:, :, :8]] + [x for x in scores if x is not None])
+    assert all(torch.equal(x, y) for x, y in zip(*runs)), width
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_can_be_captured():
+    """What a kernel is prepared with on its first launch can be done while a graph is recorded."""
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS_IN_A_GRAPH], capture_output=True, text=True, timeout=300,
+                       cwd=pathlib.Path(__file__).resolve().parents[1])
+    assert r.returncode == 0 and r.stdout.strip() == "same", r.stdout + r.stderr

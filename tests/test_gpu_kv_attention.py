@@ -287,3 +287,115 @@ def test_arguments_that_are_refused():
             call()
         assert e.value.status == status
         assert spqt.spqt_launch_count() == before
+
+
+# A table for 65536 tokens a stream: the work is then divided among all CTAs, whatever the lengths are (the tests above have few and
+# small streams, each of which a cluster of CTAs takes).
+WIDE = 2048
+
+
+@pytest.mark.parametrize("fmt,dim,group,queries", [("int8", 128, 4, 1), ("e4m3", 64, 8, 1), ("int8", 96, 3, 3), ("e4m3", 256, 5, 2)])
+@pytest.mark.parametrize("lengths", [[0], [1], [0, 1, 31, 32, 33, 0], [70, 2500, 0, 16]])
+def test_wide_tables(fmt, dim, group, queries, lengths):
+    st = Streams(lengths, 2, dim, 32, fmt, seed=41 + dim, width=WIDE)
+    compare(st, st.queries(2 * group, queries, seed=42, amplitude=2.0), accumulate=True)
+
+
+def test_wide_and_narrow_tables_agree():
+    """The same contents either way: within the tolerances of both, and rows of a table beyond a stream's blocks are not read."""
+    for lengths in ([513], [40, 300], [65] * 16):
+        st = [Streams(lengths, 1, 128, 32, "int8", seed=43, width=width) for width in (None, WIDE)]
+        q = st[0].queries(4, 1, seed=44)
+        outs = [compare(s, q, True).double() for s in st]
+        _, tol, _, _ = st[0].attention(q)
+        assert bool(((outs[0] - outs[1]).abs() <= 2 * torch.from_numpy(tol).cuda()).all())
+
+
+def test_wide_tables_in_a_graph_and_on_two_streams():
+    st = Streams([3000, 70], 2, 128, 32, "int8", seed=45, width=WIDE)
+    qs = [torch.from_numpy(st.queries(8, 1, seed=46 + i)).cuda() for i in range(2)]
+    ws = [st.workspace(8) for _ in range(2)]
+    want = [spqt.spqt_kv_attention(st.cache, q, ws[0]) for q in qs]
+    outs = [torch.zeros_like(w) for w in want]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(2):
+        with torch.cuda.graph(graphs[i], stream=streams[i]):
+            for _ in range(3):
+                spqt.spqt_kv_attention(st.cache, qs[i], ws[i], out=outs[i])
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(outs[i], want[i]) for i in range(2))
+    assert all(spqt.spqt_kv_status(w) == 0 for w in ws)
+    with torch.cuda.stream(streams[0]):      # with weights: the lengths of the replay
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=streams[0]):
+            spqt.spqt_kv_attention(st.cache, qs[0], ws[0], accumulate=True, out=outs[0])
+        g.replay()
+    torch.cuda.synchronize()
+    _, _, got, got_tol = st.attention(qs[0].cpu().numpy())
+    check(st.cache.weight, st.weight + got, got_tol)
+    st.cache.length.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.count_nonzero(outs[0]) == 0
+
+
+def test_wide_tables_whose_contents_are_refused():
+    st = Streams([100, 40, 70], 2, 128, 32, "int8", seed=47, width=WIDE)
+    q = st.queries(8, 1, seed=48)
+    want, tol, _, _ = st.attention(q)
+    qd, ws = torch.from_numpy(q).cuda(), st.workspace(8)
+    for bad in (-1, st.blocks, 1 << 30):
+        st.cache.table.copy_(torch.from_numpy(st.table))
+        st.cache.table[0, 1, 1] = bad
+        got = spqt.spqt_kv_attention(st.cache, qd, ws, accumulate=True).cpu().numpy().astype(np.float64)
+        assert spqt.spqt_kv_status(ws) == 3
+        ws.zero_()
+        assert np.isnan(got[0, 0, 4:]).all()
+        check(got[0, 0, :4], want[0, 0, :4], tol[0, 0, :4])
+        check(got[1:], want[1:], tol[1:])
+    st.cache.table.copy_(torch.from_numpy(st.table))
+    for bad in (-1, WIDE * 32 + 1, 2 ** 31 - 1):
+        st.cache.length[1, 0] = bad
+        got = spqt.spqt_kv_attention(st.cache, qd, ws).cpu().numpy().astype(np.float64)
+        assert spqt.spqt_kv_status(ws) == 3
+        ws.zero_()
+        assert (got[1, 0, :4] == 0).all()
+        check(got[0], want[0], tol[0])
+        check(got[1, 0, 4:], want[1, 0, 4:], tol[1, 0, 4:])
+
+
+def test_wide_tables_and_values_that_are_not_finite():
+    st = Streams([64 + 1], 2, 128, 16, "int8", seed=49, width=2 * WIDE)
+    q = st.queries(4, 1, seed=50)
+    st.cache.v_scale[int(st.table[0, 1, 0])] = float("nan")
+    out = attend(st, q).cpu().numpy()
+    want, tol, _, _ = st.attention(q)
+    check(out[:, :, :2].astype(np.float64), want[:, :, :2], tol[:, :, :2])
+    assert np.isnan(out[:, :, 2:]).all()
+    st = Streams([32 + 9], 1, 128, 32, "int8", seed=51, width=WIDE)
+    q = st.queries(3, 4, seed=52)
+    st.cache.v_tail[0, 0, 7, 5] = float("inf")     # token 39 of 41: seen by the queries 2 and 3
+    st.cache.k_tail[0, 0, 8] = float("nan")        # a key of the last token: seen by the last query
+    out = attend(st, q).cpu().numpy()
+    want, tol, _, _ = st.attention(q)
+    check(out[:, :2].astype(np.float64), want[:, :2], tol[:, :2])
+    assert np.isposinf(out[:, 2, :, 5]).all() and np.isfinite(np.delete(out[:, 2], 5, -1)).all() and np.isnan(out[:, 3]).all()
+
+
+def test_wide_tables_and_views():
+    st = Streams([50, 3, 129], 2, 128, 32, "int8", seed=53, width=WIDE)
+    q = st.queries(8, 2, seed=54)
+    wide = torch.full((3, 2, 8 + 4, 128), float("nan"), dtype=torch.float16, device="cuda")
+    wide[:, :, :8] = torch.from_numpy(q).cuda()
+    out = torch.full((3, 5, 8 + 3, 128), 7.0, dtype=torch.float16, device="cuda")
+    got = spqt.spqt_kv_attention(st.cache, wide[:, :, :8], st.workspace(8, 2), out=out[:, 1:3, :8])
+    torch.cuda.synchronize()
+    want, tol, _, _ = st.attention(q)
+    check(got, want, tol)
+    assert bool((out[:, 0] == 7).all() and (out[:, 3:] == 7).all() and (out[:, :, 8:] == 7).all())

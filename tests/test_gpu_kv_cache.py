@@ -340,6 +340,16 @@ def test_evict_of_the_longest_rows(width):
     check_evict(c, w, width // 2 + 1, 2, 3)
 
 
+@pytest.mark.parametrize("inner", [511, 512, 513, 2047, 2048, 2049])
+def test_evict_around_the_sizes_of_the_search(inner):
+    """As many blocks to choose among as one warp's registers, or four warps', hold, one fewer and one more."""
+    few = lambda rng, shape: np.repeat(rng.integers(0, 5, (shape[0], 1)), shape[1], 1)
+    for weight in (HEAVY, few):
+        c, w = plain_cache([(inner + 5) * 32, (inner + 5) * 32 + 7, (inner + 4) * 32 + 31], 1, 32, inner + 6, seed=inner, weight=weight)
+        for keep in (6, 5 + inner // 2, 5 + inner - 2):
+            check_evict(c, w, keep, 2, 3)
+
+
 def test_evict_refuses():
     c, w = plain_cache([40], 1, 16, 4, seed=1, weight=HEAVY)
     ws = spqt.new_kv_workspace(c, 1)
