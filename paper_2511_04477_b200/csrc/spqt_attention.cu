@@ -749,7 +749,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             // ---- the CTAs' sums: each CTA finishes its share of the rows' dimensions
             cluster_arrive_release();
             cluster_wait();
-            constexpr int kShare = ROWS * (D / 4) / kClusterCtas;
+            constexpr int kItems = ROWS * (D / 4), kShare = (kItems + kClusterCtas - 1) / kClusterCtas;
             const int rank = cta % kClusterCtas;
             auto joined = [&](int r, float2* x, float* most) {    // the CTAs' (M, l) of a row, their largest M and the sum
                 float m = -INFINITY, sum = 0.0f;
@@ -764,7 +764,7 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             };
             float2 x[kClusterCtas];
             float m;
-            if (tid < kShare) {
+            if (tid < kShare && rank * kShare + tid < kItems) {
                 const int i = rank * kShare + tid, r = i / (D / 4), d = i % (D / 4) * 4;
                 float4 y[kClusterCtas], v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -1030,13 +1030,16 @@ inline bool attention_workspace(const spqt_kv_cache& c, int group, int queries, 
     return true;
 }
 
-// Segments for which a cluster of 8 or of 4 CTAs each is taken, if `most` of them fit.  A cluster has none of the fixed cost of the division
-// of the work, of parts by way of global memory and of a kernel for the weights, but fewer SMs.  Eight streams of 512 / 2048 / 4096 /
-// 8000 tokens 5.1 / 5.5 / 7.0 / 9.9 us by clusters of 8, 7.7 / 8.9 / 9.8 / 11.4 otherwise; with weights 6.7 against 11.2 with 2048.
+// Segments for which a cluster of 16, 8 or 4 CTAs each is taken, if `most` of them fit (7, 15 and 33 on the GPU that the figures are of).
+// A cluster has none of the fixed cost of the division of the work, of parts by way of global memory and of a kernel for the weights,
+// but fewer SMs.  Eight streams of 512 / 2048 / 4096 / 8000 tokens 5.1 / 5.5 / 7.0 / 9.9 us by clusters of 8, 7.7 / 8.9 / 9.8 / 11.4
+// otherwise; with weights 6.7 against 11.2 with 2048.  Four of 512 / 2048 / 4001 / 8000 / 16000 / 32000 by clusters of 16 5.5 / 5.5 /
+// 6.0 / 7.1 / 10.2 / 16.5, of 8 or otherwise 5.1 / 5.4 / 7.3 / 10.5 / 11.7 / 14.3.
 // The lengths are on the device: what the table can hold stands for them, and where some streams are shorter the others' SMs wait.
 inline bool by_clusters(const AttnArgs& a, int ctas, int segments, int most)
 {
     if (segments > most || (a.accumulate && a.row_groups > 1)) return false;
+    if (ctas == 16) return a.most_tiles > 96 && a.most_tiles <= 600;
     if (ctas == 8) return segments <= 16 && a.most_tiles <= 512 && a.most_tiles * (150 - 8 * segments) <= 24000;
     return segments <= 32 && a.most_tiles <= 160;
 }
@@ -1066,6 +1069,7 @@ cudaError_t launch_clusters(const AttnArgs& a, int segments, cudaStream_t s, boo
     cfg.numAttrs = 1;
     if (allowed_dev != dev) {
         err = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, ROWS, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kRing);
+        if (err == cudaSuccess && CL > 8) err = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, ROWS, CL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (err != cudaSuccess) return err;
         if (cudaOccupancyMaxActiveClusters(&most, kv_attention_kernel<FMT, D, ROWS, CL>, &cfg) != cudaSuccess) {
             (void)cudaGetLastError();
@@ -1089,8 +1093,9 @@ cudaError_t launch_attention(const AttnArgs& a, cudaStream_t s)
     cudaError_t err;
     if constexpr (ROWS <= 8) {                                 // (sixteen rows are for more streams)
         bool taken = false;
-        if (segments <= 16) err = launch_clusters<FMT, D, ROWS, 8>(a, segments, s, &taken);
-        else err = cudaSuccess;
+        err = cudaSuccess;
+        if (segments <= 8) err = launch_clusters<FMT, D, ROWS, 16>(a, segments, s, &taken);
+        if (err == cudaSuccess && !taken && segments <= 16) err = launch_clusters<FMT, D, ROWS, 8>(a, segments, s, &taken);
         if (err == cudaSuccess && !taken && segments <= 32) err = launch_clusters<FMT, D, ROWS, 4>(a, segments, s, &taken);
         if (err != cudaSuccess || taken) return err;
     }

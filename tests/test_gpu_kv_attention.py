@@ -399,3 +399,11 @@ def test_wide_tables_and_views():
     want, tol, _, _ = st.attention(q)
     check(got, want, tol)
     assert bool((out[:, 0] == 7).all() and (out[:, 3:] == 7).all() and (out[:, :, 8:] == 7).all())
+
+
+@pytest.mark.parametrize("fmt,dim,group,queries", [("int8", 128, 4, 1), ("e4m3", 128, 8, 1), ("int8", 64, 5, 2), ("e4m3", 96, 1, 1), ("int8", 256, 2, 4)])
+@pytest.mark.parametrize("lengths", [[4001], [16000, 1, 0], [5000, 0, 31, 33, 127, 6001, 17]])
+def test_few_streams_of_middling_tables(fmt, dim, group, queries, lengths):
+    """One to seven streams whose tables hold 4000 to 18000 tokens: the largest clusters, where the device takes that many."""
+    st = Streams(lengths, 1, dim, 32, fmt, seed=61 + dim)
+    compare(st, st.queries(group, queries, seed=62, amplitude=2.0), accumulate=True)
