@@ -21,7 +21,7 @@
 // its tiles in turn, each with a ring of tiles on their way (cp.async, so that a block number is all that is needed ahead).  A segment
 // that lies within one CTA is finished there; of the others the CTA that comes last adds the parts, in the order of the CTAs.  Where
 // weights are accumulated, a second kernel turns the scores that the first one left into probabilities.  Few segments of caches that
-// hold little go the other way (by_clusters): a cluster of CTAs each, whose sums meet through its shared memory, weights included.
+// hold little go the other way (cluster_of): a cluster of CTAs each, whose sums meet through its shared memory, weights included.
 #include <cuda_fp8.h>
 
 #include "spqt_common.cuh"
@@ -36,6 +36,7 @@ constexpr int kTile = 32;               // tokens of a tile of codes; half as ma
 // tokens of eight streams 18.5 / 11.5 / 11.5 / 11.4, ten streams of five queries in two row groups 39.8 / 38.3 / 36.8 / 39.6.
 constexpr int kRoom = 16;
 constexpr int kMaxAttnCtas = 160;       // parts at most
+constexpr int kMostCluster = 16, kPortableCluster = 8;   // CTAs of a cluster at most; of one that every device has
 constexpr int kLengthCache = 1024;      // streams whose lengths a CTA keeps in shared memory
 constexpr float kUp = 10.0f;            // p of the largest score is 2^kUp, when M is set
 constexpr float kSlack = 4.0f;          // and 2^(kUp + kSlack) before M is set anew
@@ -51,6 +52,8 @@ struct AttnArgs {
     int shift;                          // log2 of the tokens of a block
     int accumulate;
     int most_tiles;                     // that a segment may have
+    int cluster;                        // CTAs of a cluster, where a cluster takes each segment
+    unsigned cluster_inv;               // 2^32 / cluster rounded up (cluster 1: 0)
     float scale_log2;
     int* status;
     int* begin;                         // workspace: the place of every segment's first tile, behind them the sum of tiles and rooms
@@ -171,16 +174,21 @@ __device__ __forceinline__ float4 ld_cluster_f32x4(unsigned addr)
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ unsigned cluster_rank()
+{
+    unsigned r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
 __device__ __forceinline__ void cluster_arrive_release() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 
-// CL > 0: a segment for each cluster of CL CTAs instead of parts of all of them; the CTAs' sums meet through shared memory, and the
-// weights are added here as well.  No CTA leaves early: the others may read its shared memory.
-template <int FMT, int D, int ROWS, int CL>
+// MOST > 0: a segment for each cluster of up to MOST CTAs instead of parts of all of them; the CTAs' sums meet through shared memory, and
+// the weights are added here as well.  No CTA leaves early: the others may read its shared memory.
+template <int FMT, int D, int ROWS, int MOST>
 __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attention_kernel(const AttnArgs a, int streams)
 {
     using S = AttnShape<D, ROWS>;
-    constexpr bool CLUSTER = CL > 0;
-    constexpr int kClusterCtas = CLUSTER ? CL : 1;
+    constexpr bool CLUSTER = MOST > 0;
     constexpr int NW = S::kWarps, STAGES = S::kStages, NC = S::kCols, CH = D / 16;
     extern __shared__ __align__(128) unsigned char s_ring[];                 // [NW][STAGES][kTileBytes], then s_part
     __shared__ int s_len[kLengthCache];
@@ -201,13 +209,14 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
     int t0, t1, seg0, begin0, n0, tiles0, total = 0, ctas = 0;
     auto length_of = [&](int st) { return st < kLengthCache ? s_len[st] : length_or_none((int)ld_global_u32(c.length + st), c, a.status); };
     if constexpr (CLUSTER) {
-        const int rank = cta % kClusterCtas;
-        seg0 = cta / kClusterCtas;
+        const int rank = (int)cluster_rank();
+        asm("mov.u32 %0, %%clusterid.x;" : "=r"(seg0));
         n0 = length_or_none((int)ld_global_u32(c.length + seg0 / a.row_groups), c, a.status);
         tiles0 = tiles_of(n0, shift);
         begin0 = 0;
-        t0 = tiles0 * rank / kClusterCtas;
-        t1 = tiles0 * (rank + 1) / kClusterCtas;
+        t0 = (int)__umulhi((unsigned)(tiles0 * rank), a.cluster_inv);       // tiles0 * rank / cluster (2^15 at most, so exact)
+        t1 = (int)__umulhi((unsigned)(tiles0 * (rank + 1)), a.cluster_inv);
+        if (a.cluster == 1) t1 = tiles0;
     } else {
     const int per = (streams + NW * 32 - 1) / (NW * 32);
     int mine = 0, busy = 0;
@@ -749,31 +758,38 @@ __global__ void __launch_bounds__(AttnShape<D, ROWS>::kWarps * 32, 1) kv_attenti
             // ---- the CTAs' sums: each CTA finishes its share of the rows' dimensions
             cluster_arrive_release();
             cluster_wait();
-            constexpr int kItems = ROWS * (D / 4), kShare = (kItems + kClusterCtas - 1) / kClusterCtas;
-            const int rank = cta % kClusterCtas;
-            auto joined = [&](int r, float2* x, float* most) {    // the CTAs' (M, l) of a row, their largest M and the sum
+            constexpr int kItems = ROWS * (D / 4);
+            const int rank = (int)cluster_rank(), share = (int)__umulhi((unsigned)(kItems + a.cluster - 1), a.cluster_inv) + (a.cluster == 1 ? kItems : 0);
+            // the CTAs' (M, l) of a row, their largest M and the sum.  (Places behind the last CTA read its values again, which count as
+            // none: a branch for each of them takes 1.1 us.)
+            auto joined = [&](int r, float2* x, float* most) {
                 float m = -INFINITY, sum = 0.0f;
 #pragma unroll
-                for (int k = 0; k < kClusterCtas; ++k) x[k] = ld_cluster_f32x2(cluster_map(smem_u32(&s_cta[r]), k));
+                for (int k = 0; k < MOST; ++k) {
+                    x[k] = ld_cluster_f32x2(cluster_map(smem_u32(&s_cta[r]), min(k, a.cluster - 1)));
+                    if (k >= a.cluster) x[k] = make_float2(-INFINITY, 0.0f);
+                }
 #pragma unroll
-                for (int k = 0; k < kClusterCtas; ++k) m = fmaxf(m, x[k].x);
+                for (int k = 0; k < MOST; ++k) m = fmaxf(m, x[k].x);
 #pragma unroll
-                for (int k = 0; k < kClusterCtas; ++k) sum += x[k].x == m ? x[k].y : x[k].y * exp2_fast(x[k].x - m);
+                for (int k = 0; k < MOST; ++k) sum += x[k].x == m ? x[k].y : x[k].y * exp2_fast(x[k].x - m);
                 *most = m;
                 return sum;
             };
-            float2 x[kClusterCtas];
+            float2 x[MOST > 0 ? MOST : 1];
             float m;
-            if (tid < kShare && rank * kShare + tid < kItems) {
-                const int i = rank * kShare + tid, r = i / (D / 4), d = i % (D / 4) * 4;
-                float4 y[kClusterCtas], v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = rank * share + tid; i < min(kItems, (rank + 1) * share); i += NW * 32) {
+                const int r = i / (D / 4), d = i % (D / 4) * 4;
+                float4 y[MOST > 0 ? MOST : 1], v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int k = 0; k < kClusterCtas; ++k) y[k] = ld_cluster_f32x4(cluster_map(smem_u32(&s_o[0][r][d]), k));
+                for (int k = 0; k < MOST; ++k) y[k] = ld_cluster_f32x4(cluster_map(smem_u32(&s_o[0][r][d]), min(k, a.cluster - 1)));
                 const float sum = joined(r, x, &m);
 #pragma unroll
-                for (int k = 0; k < kClusterCtas; ++k) {
+                for (int k = 0; k < MOST; ++k) {
                     const float f = x[k].x == m ? 1.0f : exp2_fast(x[k].x - m);
-                    v.x = fmaf(y[k].x, f, v.x), v.y = fmaf(y[k].y, f, v.y), v.z = fmaf(y[k].z, f, v.z), v.w = fmaf(y[k].w, f, v.w);
+                    const bool in = k < a.cluster;
+                    v.x = fmaf(in ? y[k].x : 0.0f, f, v.x), v.y = fmaf(in ? y[k].y : 0.0f, f, v.y);
+                    v.z = fmaf(in ? y[k].z : 0.0f, f, v.z), v.w = fmaf(in ? y[k].w : 0.0f, f, v.w);
                 }
                 if (row0 + r < a.rows) answer(r, d, m, sum, v);
             }
@@ -1005,7 +1021,8 @@ struct AttnWorkspace {
 };
 
 // false where the tiles' numbers would pass 31 bits
-inline int most_tiles(const spqt_kv_cache& c) { return (c.table_width * c.block_tokens + kTile - 1) / kTile + 8; }
+constexpr int kMoreTiles = 8;           // tiles of 16 tokens of a block of 128, the largest
+inline int most_tiles(const spqt_kv_cache& c) { return (c.table_width * c.block_tokens + kTile - 1) / kTile + kMoreTiles; }
 inline bool attention_workspace(const spqt_kv_cache& c, int group, int queries, AttnWorkspace* w)
 {
     const long long streams = (long long)c.batch * c.kv_heads;
@@ -1030,59 +1047,89 @@ inline bool attention_workspace(const spqt_kv_cache& c, int group, int queries, 
     return true;
 }
 
-// Segments for which a cluster of 16, 8 or 4 CTAs each is taken, if `most` of them fit (7, 15 and 33 on the GPU that the figures are of).
-// A cluster has none of the fixed cost of the division of the work, of parts by way of global memory and of a kernel for the weights,
-// but fewer SMs.  Eight streams of 512 / 2048 / 4096 / 8000 tokens 5.1 / 5.5 / 7.0 / 9.9 us by clusters of 8, 7.7 / 8.9 / 9.8 / 11.4
-// otherwise; with weights 6.7 against 11.2 with 2048.  Four of 512 / 2048 / 4001 / 8000 / 16000 / 32000 by clusters of 16 5.5 / 5.5 /
-// 6.0 / 7.1 / 10.2 / 16.5, of 8 or otherwise 5.1 / 5.4 / 7.3 / 10.5 / 11.7 / 14.3.
-// The lengths are on the device: what the table can hold stands for them, and where some streams are shorter the others' SMs wait.
-inline bool by_clusters(const AttnArgs& a, int ctas, int segments, int most)
+// CTAs of the clusters that take a segment each, 0: the work is divided among all CTAs instead.  `most`: clusters of so many CTAs that
+// fit (of 16: 7, 10: 11, 8: 15, 6: 22, 4: 33 on the GPU that the figures are of); the segments have to fit all.
+//   A cluster has none of the fixed cost of the division, of parts by way of global memory and of a kernel for the weights, but fewer
+// SMs.  Eight heads of 1 / 2 / 5 / 8 / 12 sequences of 1000 tokens by clusters 5.8 / 6.1 / 7.3 / 8.1 / 10.5 us, otherwise 8.6 / 8.9 / 10.5 /
+// 13.1 / 15.5; eight sequences with weights 9.3 against 16.1; four sequences of 2000, twelve rows, 9.7 against 15.2; four heads of 16000
+// 10.2 against 11.7.  Five tiles a warp at most: the lengths are on the device, so that what the table can hold stands for them, and
+// where one stream alone has them all, the other SMs wait (12 us, when 9 would do).
+//   Of the sizes that fit, the smallest that saves the warps a tile, but 8, or 4 for few tiles, where the warps share a scheduler less
+// (two heads of 1000 tokens by 4 6.1 us, by 8 5.5; eight of 40 5.3 and 5.6).
+inline int cluster_of(const AttnArgs& a, int warps, int segments, const int* most)
 {
-    if (segments > most || (a.accumulate && a.row_groups > 1)) return false;
-    if (ctas == 16) return a.most_tiles > 96 && a.most_tiles <= 600;
-    if (ctas == 8) return segments <= 16 && a.most_tiles <= 512 && a.most_tiles * (150 - 8 * segments) <= 24000;
-    return segments <= 32 && a.most_tiles <= 160;
+    if (a.accumulate && a.row_groups > 1) return 0;
+    const int tiles = a.most_tiles - kMoreTiles;
+    int cl = kMostCluster;
+    while (cl > 0 && most[cl] < segments) --cl;
+    if (cl == 0 || tiles > 5 * warps * cl) return 0;
+    const int each = (tiles + warps * cl - 1) / (warps * cl), fewest = (tiles + warps * each - 1) / (warps * each), least = tiles > 2 * warps ? 8 : 4;
+    return fewest > least ? fewest : cl < least ? cl : least;
 }
 
-template <int FMT, int D, int ROWS, int CL>
-cudaError_t launch_clusters(const AttnArgs& a, int segments, cudaStream_t s, bool* taken)
+template <int FMT, int D, int ROWS, int MOST>
+cudaError_t launch_clusters(const AttnArgs& a, int segments, bool prepare, cudaLaunchConfig_t cfg, cudaLaunchAttribute* attr, int* most)
 {
-    using S = AttnShape<D, ROWS>;
-    static thread_local int allowed_dev = -1, most = 0;
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess) return err;
-    if (allowed_dev == dev && !by_clusters(a, CL, segments, most)) return cudaSuccess;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(segments * CL));
-    cfg.blockDim = dim3(S::kWarps * 32);
-    cfg.dynamicSmemBytes = S::kRing;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
+    const auto kernel = kv_attention_kernel<FMT, D, ROWS, MOST>;
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CL;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (allowed_dev != dev) {
-        err = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, ROWS, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kRing);
-        if (err == cudaSuccess && CL > 8) err = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, ROWS, CL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (prepare) {                          // most[cl]: clusters of so many CTAs that fit, for the sizes that are this kernel's
+        cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+        if (err == cudaSuccess && MOST > kPortableCluster) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (err != cudaSuccess) return err;
-        if (cudaOccupancyMaxActiveClusters(&most, kv_attention_kernel<FMT, D, ROWS, CL>, &cfg) != cudaSuccess) {
-            (void)cudaGetLastError();
-            most = 0;
+        cfg.numAttrs = 1;
+        for (int cl = MOST == 4 ? 1 : MOST / 2 + 1; cl <= MOST; ++cl) {
+            attr[0].val.clusterDim.x = cl;
+            cfg.gridDim = dim3((unsigned)cl);
+            if (cudaOccupancyMaxActiveClusters(&most[cl], kernel, &cfg) != cudaSuccess) {
+                (void)cudaGetLastError();
+                most[cl] = 0;
+            }
         }
-        allowed_dev = dev;
-        if (!by_clusters(a, CL, segments, most)) return cudaSuccess;
+        return cudaSuccess;
     }
+    attr[0].val.clusterDim.x = a.cluster;
+    cfg.gridDim = dim3((unsigned)(segments * a.cluster));
     cfg.numAttrs = g_no_pdl ? 1 : 2;
-    err = cudaLaunchKernelEx(&cfg, kv_attention_kernel<FMT, D, ROWS, CL>, a, a.c.batch * a.c.kv_heads);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, a, a.c.batch * a.c.kv_heads);
     if (err == cudaSuccess) count_launch();
-    *taken = true;
     return err;
+}
+
+// *taken: whether the call went by clusters.
+template <int FMT, int D, int ROWS>
+cudaError_t try_clusters(AttnArgs a, int segments, cudaStream_t s, bool* taken)
+{
+    using S = AttnShape<D, ROWS>;
+    static thread_local int prepared_dev = -1, most[kMostCluster + 1];
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(S::kWarps * 32);
+    cfg.dynamicSmemBytes = S::kRing;
+    cfg.stream = s;
+    constexpr bool kLarge = ROWS < 16;      // (sixteen rows are for more streams than there are clusters of more than 8)
+    if (prepared_dev != dev) {
+        err = launch_clusters<FMT, D, ROWS, 4>(a, segments, true, cfg, attr, most);
+        if (err == cudaSuccess) err = launch_clusters<FMT, D, ROWS, 8>(a, segments, true, cfg, attr, most);
+        if constexpr (kLarge)
+            if (err == cudaSuccess) err = launch_clusters<FMT, D, ROWS, 16>(a, segments, true, cfg, attr, most);
+        if (err != cudaSuccess) return err;
+        prepared_dev = dev;
+    }
+    a.cluster = cluster_of(a, S::kWarps, segments, most);
+    *taken = a.cluster > 0;
+    if (!*taken) return cudaSuccess;
+    a.cluster_inv = a.cluster == 1 ? 0u : (unsigned)(((1ULL << 32) + a.cluster - 1) / a.cluster);
+    if constexpr (kLarge)
+        if (a.cluster > 8) return launch_clusters<FMT, D, ROWS, 16>(a, segments, false, cfg, attr, most);
+    return a.cluster > 4 ? launch_clusters<FMT, D, ROWS, 8>(a, segments, false, cfg, attr, most) : launch_clusters<FMT, D, ROWS, 4>(a, segments, false, cfg, attr, most);
 }
 
 template <int FMT, int D, int ROWS>
@@ -1090,15 +1137,9 @@ cudaError_t launch_attention(const AttnArgs& a, cudaStream_t s)
 {
     using S = AttnShape<D, ROWS>;
     const int streams = a.c.batch * a.c.kv_heads, segments = streams * a.row_groups;
-    cudaError_t err;
-    if constexpr (ROWS <= 8) {                                 // (sixteen rows are for more streams)
-        bool taken = false;
-        err = cudaSuccess;
-        if (segments <= 8) err = launch_clusters<FMT, D, ROWS, 16>(a, segments, s, &taken);
-        if (err == cudaSuccess && !taken && segments <= 16) err = launch_clusters<FMT, D, ROWS, 8>(a, segments, s, &taken);
-        if (err == cudaSuccess && !taken && segments <= 32) err = launch_clusters<FMT, D, ROWS, 4>(a, segments, s, &taken);
-        if (err != cudaSuccess || taken) return err;
-    }
+    bool taken = false;
+    cudaError_t err = try_clusters<FMT, D, ROWS>(a, segments, s, &taken);
+    if (err != cudaSuccess || taken) return err;
     static thread_local int allowed_dev = -1;
     int dev = 0;
     err = cudaGetDevice(&dev);
@@ -1179,7 +1220,7 @@ spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long lo
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     const int group = q_heads / cache->kv_heads, rows = group * queries, R = rows_of(rows, (long long)cache->batch * cache->kv_heads);
     const AttnArgs a = {*cache, static_cast<const __half*>(q), q_batch_stride, q_token_stride, static_cast<__half*>(out), out_batch_stride, out_token_stride,
-                        group, queries, rows, (rows + R - 1) / R, 31 - __builtin_clz((unsigned)cache->block_tokens), accumulate ? 1 : 0, most_tiles(*cache), scale * 1.4426950408889634f, static_cast<int*>(status_word(workspace)),
+                        group, queries, rows, (rows + R - 1) / R, 31 - __builtin_clz((unsigned)cache->block_tokens), accumulate ? 1 : 0, most_tiles(*cache), 0, 0u, scale * 1.4426950408889634f, static_cast<int*>(status_word(workspace)),
                         reinterpret_cast<int*>(ws + w.begin), reinterpret_cast<int*>(ws + w.arrived), reinterpret_cast<float2*>(ws + w.ml),
                         reinterpret_cast<float*>(ws + w.o), reinterpret_cast<float2*>(ws + w.lse), reinterpret_cast<int4*>(ws + w.tiles),
                         reinterpret_cast<float*>(ws + w.scores)};

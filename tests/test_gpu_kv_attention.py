@@ -407,3 +407,23 @@ def test_few_streams_of_middling_tables(fmt, dim, group, queries, lengths):
     """One to seven streams whose tables hold 4000 to 18000 tokens: the largest clusters, where the device takes that many."""
     st = Streams(lengths, 1, dim, 32, fmt, seed=61 + dim)
     compare(st, st.queries(group, queries, seed=62, amplitude=2.0), accumulate=True)
+
+
+@pytest.mark.parametrize("fmt,dim,bt", [("int8", 128, 32), ("e4m3", 64, 16), ("int8", 96, 64), ("e4m3", 256, 128)])
+@pytest.mark.parametrize("group,queries", [(4, 1), (16, 1), (3, 4), (8, 3)])
+def test_wide_tables_of_many_streams(fmt, dim, bt, group, queries):
+    lengths = [0, 1, 2, 16, 17, 40, 130, 333, 500, 1025]
+    st = Streams(lengths, 2, dim, bt, fmt, seed=65 + group, width=65536 // bt)
+    compare(st, st.queries(2 * group, queries, seed=66, amplitude=1.5), accumulate=True)
+
+
+@pytest.mark.parametrize("streams", [9, 16, 23, 34, 50, 75, 148, 149])
+@pytest.mark.parametrize("fmt,dim,group,queries", [("int8", 128, 4, 1), ("e4m3", 64, 8, 2), ("int8", 256, 5, 3)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_numbers_of_streams(streams, fmt, dim, group, queries, accumulate):
+    """Clusters of every size, down to one CTA, and one stream more than the device has SMs."""
+    rng = np.random.Generator(np.random.PCG64(streams))
+    lengths = rng.integers(0, 400, streams) * (rng.random(streams) < 0.9)
+    lengths[0] = 500
+    st = Streams(lengths, 1, dim, 32, fmt, seed=67 + streams)
+    compare(st, st.queries(group, queries, seed=68, amplitude=2.0), accumulate)
