@@ -159,3 +159,69 @@ def test_refusals():
     empty = spqt.spqt_token_logprobs(x[:0], t[:0], top=4)
     assert [tuple(v.shape) for v in empty] == [(0,), (0,), (0, 4), (0, 4)]
     assert spqt.spqt_launch_count() == before
+
+
+# Rows of a warp, of 128 threads, of 256, of a cluster: (rows, vocab) with 16-bit logits, with fp32.
+SHAPES = {"warp": ((9, 1500), (9, 1500)), "team": ((9, 8000), (9, 4000)), "cta": ((301, 40000), (301, 20000)), "cluster": ((9, 128256), (9, 128256))}
+
+
+def check_shifted(x, tokens, top):
+    """As check, from logits less their row's maximum, which fp64 holds where x - log sum exp(x) has no digits left (x = -3.4e38).
+    The kernel takes the same difference: log probabilities and entropy keep check's tolerances."""
+    logprob, entropy, best, index = (t.cpu() for t in spqt.spqt_token_logprobs(x, tokens, top=top))
+    d = x.double().cpu()
+    order = torch.sort(d, dim=1, descending=True, stable=True)[1][:, :top]
+    d = d - d.max(1, keepdim=True)[0]
+    logp = d - torch.logsumexp(d, 1, keepdim=True)
+    want = torch.gather(logp, 1, tokens.cpu().long()[:, None])[:, 0]
+    assert bool((off(logprob, want) <= 2.0 ** -15 + 2.0 ** -22 * want.abs()).all()), (logprob, want)
+    p = torch.exp(logp)
+    want = -(p * torch.where(p > 0, logp, torch.zeros_like(p))).sum(1)
+    assert bool(((entropy.double() - want).abs() <= 2.0 ** -15 + 2.0 ** -17 * want).all()), (entropy, want)
+    assert torch.equal(index.long(), order)
+    want = torch.gather(logp, 1, order)
+    assert bool((off(best, want) <= 2.0 ** -15 + 2.0 ** -22 * want.abs()).all()), (best, want)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_logits_masked_with_the_lowest_values_of_the_type(dtype, shape):
+    """Finite masks: what is masked has no share in the entropy, wherever the few ordinary values of a row are.  (A sum that has
+    met only masked values moves to an ordinary maximum over a distance that times the sum's count has no finite value.)"""
+    rows, vocab = SHAPES[shape][dtype == "fp32"]
+    x = logits(rows, vocab, dtype, seed=41)
+    lowest = torch.finfo(TYPES[dtype]).min
+    second = lowest if dtype == "fp16" else -1e38
+    masked = torch.full_like(x, lowest)
+    masked[1::2] = second
+    masked[2::5, ::3] = second
+    masked[4::5, ::7] = -float("inf")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(42)
+    stays = torch.rand((rows, vocab), generator=g, device="cuda") < 0.01
+    for row, where in ((0, slice(0, 6)), (1, slice(vocab // 2, vocab // 2 + 6)), (2, slice(vocab - 6, vocab)), (3, slice(vocab - 1, vocab)), (4, slice(0, 0)), (5, slice(0, 1))):
+        stays[row] = False
+        stays[row, where] = True
+    x = torch.where(stays, x, masked)
+    tokens = torch.full((rows,), vocab // 2, dtype=torch.int32, device="cuda")
+    check_shifted(x, tokens, 5)
+    check_shifted(x, tokens, 0)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_logits_further_apart_than_the_largest_value(dtype, shape):
+    """The difference of two logits overflows: the lower ones have probability zero."""
+    rows, vocab = SHAPES[shape][dtype == "fp32"]
+    x = torch.full((rows, vocab), -3e38, dtype=TYPES[dtype], device="cuda")
+    high = [0, vocab // 2, vocab - 1]
+    for r in range(rows):
+        x[r, high[:r % 3 + 1]] = 3e38
+    logprob, entropy, best, index = spqt.spqt_token_logprobs(x, torch.zeros(rows, dtype=torch.int32, device="cuda"), top=3)
+    want = torch.log(torch.arange(rows, device="cuda") % 3 + 1.0)
+    # (equal terms: a logarithm, off by 2^-22 of it, and nothing else)
+    assert not bool(torch.isnan(entropy).any()), entropy
+    assert bool(((entropy - want).abs() <= 2.0 ** -20).all()) and bool(((logprob + want).abs() <= 2.0 ** -20).all())
+    for r in range(rows):
+        n = r % 3 + 1
+        assert index[r, :n].tolist() == high[:n] and bool(((best[r, :n] + want[r]).abs() <= 2.0 ** -20).all()) and bool(torch.isneginf(best[r, n:]).all())
