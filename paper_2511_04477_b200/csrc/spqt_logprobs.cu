@@ -470,7 +470,7 @@ struct LogAnswer {
 // Rows one after the other, a team of threads each: the values of the next 4 vectors of a thread, be they of the next row, are on
 // their way while those before are added or the row is finished.
 template <class T, int TEAM>
-__global__ void __launch_bounds__(256, 4) token_logprobs_rows_kernel(const LogArgs a, int rows)
+__global__ void __launch_bounds__(256, 4) token_logprobs_rows_kernel(const LogArgs a, unsigned rows)
 {
     constexpr int kTeams = 256 / TEAM, kList = TEAM == 32 ? 256 : TEAM == 128 ? 1024 : kLogList;
     __shared__ LogShared<TEAM / 32, kList> shared[kTeams];
@@ -480,8 +480,9 @@ __global__ void __launch_bounds__(256, 4) token_logprobs_rows_kernel(const LogAr
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const T* const logits = static_cast<const T*>(a.logits);
     uint4 w[kVecs];
-    int r = blockIdx.x * kTeams + which;
-    const int step = gridDim.x * kTeams;
+    // (unsigned: a row number plus a step passes 2^31 where there are nearly so many rows)
+    unsigned r = blockIdx.x * kTeams + which;
+    const unsigned step = gridDim.x * kTeams;
     if (r < rows) team.load(w, LogPart<T>(logits + (long long)r * a.row_stride, a.vocab), tid);
     for (; r < rows; r += step) {
         const LogPart<T> part(logits + (long long)r * a.row_stride, a.vocab);
@@ -577,7 +578,7 @@ cudaError_t launch_logprobs(LogArgs a, int rows, cudaStream_t s)
     while (ctas < kMaxLogCtas && (long long)rows * ctas < 2 * sms && part_of(2 * ctas) >= kPartThreads * V) ctas *= 2;
     if (ctas == 1) {
         auto rows_by = [&](auto kernel, int team) {
-            const int teams = 256 / team, grid = (rows + teams - 1) / teams;
+            const int teams = 256 / team, grid = (rows - 1) / teams + 1;
             return launch_overlapping(kernel, dim3(grid < 4 * sms ? grid : 4 * sms), 256, 0, s, a, rows);
         };
         // 2000 x 8000 fp16, top 20, a warp / 128 threads a row: 24.3 / 19.3 us; 4096 x 8000: 22.4 / 31.1; 1000 x 2000: 5.7 / 7.0; 1000 x 4000: 13.5 / 8.1.

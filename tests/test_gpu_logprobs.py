@@ -225,3 +225,23 @@ def test_logits_further_apart_than_the_largest_value(dtype, shape):
     for r in range(rows):
         n = r % 3 + 1
         assert index[r, :n].tolist() == high[:n] and bool(((best[r, :n] + want[r]).abs() <= 2.0 ** -20).all()) and bool(torch.isneginf(best[r, n:]).all())
+
+
+def test_as_many_rows_as_a_whole_number_counts():
+    """2^31 - 1 rows of one value: every row is answered once, and nothing in front of the first or behind the last."""
+    rows, far = 2 ** 31 - 1, 4096
+    buf = torch.zeros(far + rows + far, dtype=torch.float16, device="cuda")
+    odd = [0, 1, 4735, 4736, rows - 4737, rows - 4736, rows - 2, rows - 1]
+    for r in odd:
+        buf[far + r] = float("nan")
+    out = torch.full((rows,), 7.0, device="cuda")       # (what the answers' memory holds, if they get this)
+    del out
+    entropy = spqt.spqt_token_logprobs(buf[far:far + rows].view(rows, 1))[1]
+    assert entropy.shape == (rows,)
+    found = []
+    for at in range(0, rows, 1 << 28):
+        part = entropy[at:at + (1 << 28)]
+        nan = torch.isnan(part)
+        found += (nan.nonzero().flatten() + at).tolist()
+        assert bool((nan | (part == 0)).all())
+    assert found == odd
