@@ -66,8 +66,8 @@ __device__ __forceinline__ void move_to(Sums& a, float m)   // to a maximum not 
 {
     if (a.m == m) return;
     const float d = a.m - m, f = exp_of(d);
-    // (f = 0: nothing is left of the sums, and s * d, with masks of the type's lowest value, may be infinite)
-    a.t = a.s == 0.0f || f == 0.0f ? 0.0f : fmaf(a.s, d, a.t) * f;
+    // (f = 0: nothing summed, or nothing is left of the sums; s * d, with masks of the type's lowest value, may then be infinite)
+    a.t = f == 0.0f ? 0.0f : fmaf(a.s, d, a.t) * f;
     a.s *= f;
     a.m = m;
 }
