@@ -6,6 +6,9 @@ entry point of the same name and raises :class:`SpqtError` on a non-zero status.
 The per-token calls and the conversions do this in a native module
 (``csrc/spqt_python.cpp``), the rest through ctypes.  No arithmetic of the method happens in Python and there is no CPU fallback: if
 ``libspqt.so`` has not been built, the first call raises.
+
+A call runs on the current stream, or on ``stream`` where one is given.  The tensors that it makes are that stream's, as if it were
+the current one; what it is given has to be there when that stream comes to it.
 """
 from __future__ import annotations
 
@@ -155,6 +158,20 @@ def _stream(stream) -> int:
     return int(s.cuda_stream)
 
 
+def _new(stream, device, make, *args, **kw) -> torch.Tensor:
+    """A tensor for a call on ``stream``: of that stream's pool, made on it, and known to the current one, where the caller may read it."""
+    if stream is None:
+        return make(*args, device=device, **kw)
+    current = torch.cuda.current_stream(device)
+    handle = int(stream.cuda_stream)
+    if handle == int(current.cuda_stream):
+        return make(*args, device=device, **kw)
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)):
+        t = make(*args, device=device, **kw)
+    t.record_stream(current)
+    return t
+
+
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % name)
@@ -215,7 +232,7 @@ def spqt_pack(W: torch.Tensor, bits: int = 4, group: int = 128, stream=None) -> 
 
 
 def spqt_unpack(p: Packed, stream=None) -> torch.Tensor:
-    q = torch.empty((p.m, p.n), dtype=torch.uint8, device=p.codes.device)
+    q = _new(stream, p.codes.device, torch.empty, (p.m, p.n), dtype=torch.uint8)
     _ok(lib().spqt_unpack(_dev(p.codes, torch.uint8, "codes"), p.m, p.n, p.bits, p.group,
                           q.data_ptr(), _stream(stream)), "spqt_unpack")
     return q
@@ -397,8 +414,8 @@ def spqt_rowwise_pack(W: torch.Tensor, bits: int = 4, group: int = 128, stream=N
         raise TypeError("W must be a CUDA float16 tensor")
     m, n = W.shape
     cb, sb = spqt_rowwise_packed_sizes(m, n, bits, group)
-    codes = torch.empty(cb, dtype=torch.uint8, device=W.device)
-    scale_zero = torch.empty(sb // 2, dtype=torch.float16, device=W.device)
+    codes = _new(stream, W.device, torch.empty, cb, dtype=torch.uint8)
+    scale_zero = _new(stream, W.device, torch.empty, sb // 2, dtype=torch.float16)
     _ok(lib().spqt_rowwise_pack(W.data_ptr(), m, n, W.stride(0), bits, group, codes.data_ptr(),
                                 scale_zero.data_ptr(), _stream(stream)), "spqt_rowwise_pack")
     return RowwisePacked(codes, scale_zero, m, n, bits, group)
@@ -406,7 +423,7 @@ def spqt_rowwise_pack(W: torch.Tensor, bits: int = 4, group: int = 128, stream=N
 
 def spqt_rowwise_dense_gemv(p: RowwisePacked, x: torch.Tensor, y: torch.Tensor = None, stream=None) -> torch.Tensor:
     if y is None:
-        y = torch.empty(p.m, dtype=torch.float16, device=x.device)
+        y = _new(stream, x.device, torch.empty, p.m, dtype=torch.float16)
     _ok(lib().spqt_rowwise_dense_gemv(
         _dev(p.codes, torch.uint8, "codes"), _dev(p.scale_zero, torch.float16, "scale_zero"), p.m, p.n, p.bits, p.group,
         _dev(x, torch.float16, "x"), _dev(y, torch.float16, "y"), _stream(stream)), "spqt_rowwise_dense_gemv")
@@ -469,7 +486,7 @@ def spqt_kq_dense_gemv(p: KqPacked, x: torch.Tensor, workspace: torch.Tensor, y:
 
 def spqt_rowwise_thresholded_gemv(p: RowwisePacked, x: torch.Tensor, t: float, y: torch.Tensor = None, stream=None) -> torch.Tensor:
     if y is None:
-        y = torch.empty(p.m, dtype=torch.float16, device=x.device)
+        y = _new(stream, x.device, torch.empty, p.m, dtype=torch.float16)
     _ok(lib().spqt_rowwise_thresholded_gemv(
         _dev(p.codes, torch.uint8, "codes"), _dev(p.scale_zero, torch.float16, "scale_zero"), p.m, p.n, p.bits, p.group,
         _dev(x, torch.float16, "x"), float(t), _dev(y, torch.float16, "y"), _stream(stream)), "spqt_rowwise_thresholded_gemv")
@@ -479,9 +496,9 @@ def spqt_rowwise_thresholded_gemv(p: RowwisePacked, x: torch.Tensor, t: float, y
 def spqt_autotune(p: Packed, x: torch.Tensor, t: float, workspace: torch.Tensor, flush: torch.Tensor = None, stream=None):
     """Profile grid sizes for this shape and keep the fastest -> (ctas for the sparse calls, ctas for the dense call).
     ``flush``: an optional uint8 buffer larger than L2, rewritten before every timed launch.  Synchronises."""
-    idx = torch.empty(p.n, dtype=torch.int32, device=x.device)
-    count = torch.empty(1, dtype=torch.int32, device=x.device)
-    y = torch.empty(p.m, dtype=torch.float16, device=x.device)
+    idx = _new(stream, x.device, torch.empty, p.n, dtype=torch.int32)
+    count = _new(stream, x.device, torch.empty, 1, dtype=torch.int32)
+    y = _new(stream, x.device, torch.empty, p.m, dtype=torch.float16)
     a, b = ctypes.c_int(0), ctypes.c_int(0)
     _ok(lib().spqt_autotune(
         _dev(p.codes, torch.uint8, "codes"), _dev(p.scale_zero, torch.float16, "scale_zero"), p.m, p.n, p.bits, p.group,
@@ -501,9 +518,9 @@ def spqt_calibrate_threshold(x: torch.Tensor, sparsity: float, workspace: torch.
                              threshold: torch.Tensor = None, stream=None) -> torch.Tensor:
     """Nearest-rank threshold of |x| over a pool of fp16 calibration activations -> float32[1] on the device."""
     if workspace is None:
-        workspace = new_calibration_workspace(x.device)
+        workspace = _new(stream, x.device, new_calibration_workspace)
     if threshold is None:
-        threshold = torch.empty(1, dtype=torch.float32, device=x.device)
+        threshold = _new(stream, x.device, torch.empty, 1, dtype=torch.float32)
     _ok(lib().spqt_calibrate_threshold(
         _dev(x, torch.float16, "x") if x.numel() else None, x.numel(), float(sparsity),
         _dev(threshold, torch.float32, "threshold"), _dev(workspace, torch.int32, "workspace"), workspace.numel() * 4,

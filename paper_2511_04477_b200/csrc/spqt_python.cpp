@@ -14,6 +14,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -101,15 +102,28 @@ void* stream_of(PyObject* o)
     return v;
 }
 
-at::Tensor empty(at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& like)
+// A new tensor for a call on `stream` (an argument, which may be None).  Where that is not the current stream the memory is of
+// its pool, as if it were: memory of the current stream's pool may still be in use there, and would be given away again while the
+// call writes it.  The current stream, on which the caller may read the result, is made known as well.
+at::Tensor empty(at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& like, PyObject* stream)
 {
+    if (stream != Py_None) {
+        const auto current = c10::cuda::getCurrentCUDAStream(like.get_device());
+        const auto other = static_cast<cudaStream_t>(stream_of(stream));
+        if (other != current.stream()) {
+            const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(other, like.get_device()));
+            at::Tensor t = at::detail::empty_cuda(shape, dtype, like.device(), std::nullopt);
+            if (t.numel() > 0) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+            return t;
+        }
+    }
     return at::detail::empty_cuda(shape, dtype, like.device(), std::nullopt);
 }
 
 // The tensor an optional argument names, or a new one.
-at::Tensor given_or_empty(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype, const char* name, const at::Tensor& like)
+at::Tensor given_or_empty(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype, const char* name, const at::Tensor& like, PyObject* stream)
 {
-    return o == Py_None ? empty(shape, dtype, like) : tensor_of(o, dtype, name);
+    return o == Py_None ? empty(shape, dtype, like, stream) : tensor_of(o, dtype, name);
 }
 
 // A tensor argument as it goes back to the caller: the object that came in, or the new tensor.
@@ -192,8 +206,8 @@ PyObject* sparsify(PyObject*, Args a, Py_ssize_t na)
         const at::Tensor& x = tensor_of(a[0], at::kHalf, "x");
         const float t = float_of(a[1]);
         const int64_t n = x.numel();
-        at::Tensor idx = given_or_empty(a[2], {n > 0 ? n : 1}, at::kInt, "idx", x);
-        at::Tensor count = given_or_empty(a[3], {1}, at::kInt, "count", x);
+        at::Tensor idx = given_or_empty(a[2], {n > 0 ? n : 1}, at::kInt, "idx", x, a[4]);
+        at::Tensor count = given_or_empty(a[3], {1}, at::kInt, "count", x, a[4]);
         if (idx.numel() < n) raise(PyExc_ValueError, "%s", "idx must hold n entries");
         void* s = stream_of(a[4]);
         call("spqt_sparsify", [&] { return spqt_sparsify(x.data_ptr(), (int)n, t, (int32_t*)idx.data_ptr(), (int32_t*)count.data_ptr(), s); });
@@ -208,7 +222,7 @@ PyObject* sparse_gemv(PyObject*, Args a, Py_ssize_t na)
         need_args(na, 7);
         const Zigzag p(a[0]);
         const at::Tensor& x = tensor_of(a[1], at::kHalf, "x");
-        at::Tensor y = given_or_empty(a[5], {p.m}, at::kHalf, "y", x);
+        at::Tensor y = given_or_empty(a[5], {p.m}, at::kHalf, "y", x, a[6]);
         if (x.numel() != p.n || y.numel() != p.m) raise(PyExc_ValueError, "%s", "x must have n entries and y m entries");
         const at::Tensor& idx = tensor_of(a[2], at::kInt, "idx");
         const at::Tensor& count = tensor_of(a[3], at::kInt, "count");
@@ -231,9 +245,9 @@ PyObject* sparsify_gemv(PyObject*, Args a, Py_ssize_t na)
         const at::Tensor& x = tensor_of(a[1], at::kHalf, "x");
         const float t = float_of(a[2]);
         const at::Tensor& ws = tensor_of(a[3], at::kByte, "workspace");
-        at::Tensor idx = given_or_empty(a[4], {p.n}, at::kInt, "idx", x);
-        at::Tensor count = given_or_empty(a[5], {1}, at::kInt, "count", x);
-        at::Tensor y = given_or_empty(a[6], {p.m}, at::kHalf, "y", x);
+        at::Tensor idx = given_or_empty(a[4], {p.n}, at::kInt, "idx", x, a[7]);
+        at::Tensor count = given_or_empty(a[5], {1}, at::kInt, "count", x, a[7]);
+        at::Tensor y = given_or_empty(a[6], {p.m}, at::kHalf, "y", x, a[7]);
         if (x.numel() != p.n || y.numel() != p.m || idx.numel() < p.n)
             raise(PyExc_ValueError, "%s", "x and idx must have n entries and y m entries");
         void* s = stream_of(a[7]);
@@ -252,7 +266,7 @@ PyObject* dense_gemv(PyObject*, Args a, Py_ssize_t na)
         need_args(na, 5);
         const Zigzag p(a[0]);
         const at::Tensor& x = tensor_of(a[1], at::kHalf, "x");
-        at::Tensor y = given_or_empty(a[3], {p.m}, at::kHalf, "y", x);
+        at::Tensor y = given_or_empty(a[3], {p.m}, at::kHalf, "y", x, a[4]);
         if (x.numel() != p.n || y.numel() != p.m) raise(PyExc_ValueError, "%s", "x must have n entries and y m entries");
         const at::Tensor& ws = tensor_of(a[2], at::kByte, "workspace");
         void* s = stream_of(a[4]);
@@ -265,14 +279,14 @@ PyObject* dense_gemv(PyObject*, Args a, Py_ssize_t na)
 }
 
 // X [batch <= 8][n] with unit column stride, and Y [batch][m], given or new
-at::Tensor batch_output(const Zigzag& p, PyObject* X_o, PyObject* Y_o)
+at::Tensor batch_output(const Zigzag& p, PyObject* X_o, PyObject* Y_o, PyObject* stream)
 {
     if (!THPVariable_Check(X_o)) raise(PyExc_TypeError, "%s", "X and Y must be CUDA float16 tensors");
     const at::Tensor& X = THPVariable_Unpack(X_o);
     if (X.dim() != 2 || X.stride(1) != 1 || X.size(1) != p.n || X.size(0) < 1 || X.size(0) > 8)
         raise(PyExc_ValueError, "%s", "X must be [batch <= 8][n] with unit column stride");
     if (X.scalar_type() != at::kHalf || !X.is_cuda()) raise(PyExc_TypeError, "%s", "X and Y must be CUDA float16 tensors");
-    if (Y_o == Py_None) return empty({X.size(0), p.m}, at::kHalf, X);
+    if (Y_o == Py_None) return empty({X.size(0), p.m}, at::kHalf, X, stream);
     if (!THPVariable_Check(Y_o)) raise(PyExc_TypeError, "%s", "X and Y must be CUDA float16 tensors");
     const at::Tensor& Y = THPVariable_Unpack(Y_o);
     if (Y.scalar_type() != at::kHalf || !Y.is_cuda()) raise(PyExc_TypeError, "%s", "X and Y must be CUDA float16 tensors");
@@ -287,12 +301,12 @@ PyObject* sparse_gemm_small(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         need_args(na, 8);
         const Zigzag p(a[0]);
-        at::Tensor Y = batch_output(p, a[1], a[6]);
+        at::Tensor Y = batch_output(p, a[1], a[6], a[7]);
         const at::Tensor& X = THPVariable_Unpack(a[1]);
         const float t = float_of(a[2]);
         const at::Tensor& ws = tensor_of(a[3], at::kByte, "workspace");
-        at::Tensor idx = given_or_empty(a[4], {p.n}, at::kInt, "idx", X);
-        at::Tensor count = given_or_empty(a[5], {1}, at::kInt, "count", X);
+        at::Tensor idx = given_or_empty(a[4], {p.n}, at::kInt, "idx", X, a[7]);
+        at::Tensor count = given_or_empty(a[5], {1}, at::kInt, "count", X, a[7]);
         void* s = stream_of(a[7]);
         call("spqt_sparse_gemm_small", [&] {
             return spqt_sparse_gemm_small(p.codes, p.scale_zero, p.m, p.n, p.bits, p.group, X.data_ptr(), (int)X.stride(0), (int)X.size(0), t,
@@ -309,7 +323,7 @@ PyObject* dense_gemm_small(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         need_args(na, 5);
         const Zigzag p(a[0]);
-        at::Tensor Y = batch_output(p, a[1], a[3]);
+        at::Tensor Y = batch_output(p, a[1], a[3], a[4]);
         const at::Tensor& X = THPVariable_Unpack(a[1]);
         const at::Tensor& ws = tensor_of(a[2], at::kByte, "workspace");
         void* s = stream_of(a[4]);
@@ -332,7 +346,7 @@ PyObject* kqw_gemv(PyObject*, Args a, Py_ssize_t na)
         const void* records = tensor_attr(p, g_names.records, at::kByte, "records").data_ptr();
         const int m = int_attr(p, g_names.m), n = int_attr(p, g_names.n), bits = int_attr(p, g_names.bits);
         const at::Tensor& x = tensor_of(a[1], at::kHalf, "x");
-        at::Tensor y = given_or_empty(rest[1], {m}, at::kHalf, "y", x);
+        at::Tensor y = given_or_empty(rest[1], {m}, at::kHalf, "y", x, rest[2]);
         const at::Tensor& ws = tensor_of(rest[0], at::kByte, "workspace");
         void* s = stream_of(rest[2]);
         const char* where = PyUnicode_AsUTF8(rest[3]);
@@ -372,7 +386,7 @@ PyObject* pack(PyObject*, Args a, Py_ssize_t na)
         const int m = (int)W.size(0), n = (int)W.size(1), bits = int_of(a[1]), group = int_of(a[2]);
         size_t cb = 0, sb = 0;
         check(spqt_packed_sizes(m, n, bits, group, &cb, &sb, nullptr), "spqt_packed_sizes");
-        at::Tensor codes = empty({(int64_t)cb}, at::kByte, W), sz = empty({(int64_t)(sb / 2)}, at::kHalf, W);
+        at::Tensor codes = empty({(int64_t)cb}, at::kByte, W, a[3]), sz = empty({(int64_t)(sb / 2)}, at::kHalf, W, a[3]);
         void* s = stream_of(a[3]);
         call("spqt_pack", [&] { return spqt_pack(W.data_ptr(), m, n, (int)W.stride(0), bits, group, codes.data_ptr(), sz.data_ptr(), s); });
         return tuple_of(hand_back(Py_None, codes), hand_back(Py_None, sz));
@@ -390,7 +404,7 @@ PyObject* kqw_pack(PyObject*, Args a, Py_ssize_t na)
         if (!where) throw Raised();
         size_t rb = 0;
         check(spqt_kqw_packed_sizes(m, n, bits, &rb, nullptr), "spqt_kqw_packed_sizes");
-        at::Tensor records = empty({(int64_t)rb}, at::kByte, W);
+        at::Tensor records = empty({(int64_t)rb}, at::kByte, W, a[2]);
         void* s = stream_of(a[2]);
         call(where, [&] { return spqt_kqw_pack(W.data_ptr(), m, n, (int)W.stride(0), bits, records.data_ptr(), s); });
         return hand_back(Py_None, records);
@@ -534,7 +548,7 @@ PyObject* kv_attention(PyObject*, Args a, Py_ssize_t na)
         if (accumulate < 0) throw Raised();
         at::Tensor out;
         if (a[5] == Py_None) {
-            out = empty(q.sizes(), at::kHalf, q);
+            out = empty(q.sizes(), at::kHalf, q, a[6]);
         } else {
             out = p.rows(a[5], q.size(2), "out");
             if (out.size(1) != q.size(1)) raise(PyExc_ValueError, "%s", "out must have the shape of q");
@@ -591,10 +605,10 @@ PyObject* token_logprobs(PyObject*, Args a, Py_ssize_t na)
             const at::Tensor& k = tensor_of(a[1], at::kInt, "tokens");
             if (k.dim() != 1 || k.size(0) != rows || k.get_device() != x.get_device()) raise(PyExc_ValueError, "%s", "tokens must be [rows] on the device of logits");
             tokens = static_cast<const int32_t*>(k.data_ptr());
-            logprob = empty({rows}, at::kFloat, x);
+            logprob = empty({rows}, at::kFloat, x, a[4]);
         }
-        if (wants_entropy) entropy = empty({rows}, at::kFloat, x);
-        at::Tensor best = empty({rows, top}, at::kFloat, x), index = empty({rows, top}, at::kInt, x);
+        if (wants_entropy) entropy = empty({rows}, at::kFloat, x, a[4]);
+        at::Tensor best = empty({rows, top}, at::kFloat, x, a[4]), index = empty({rows, top}, at::kInt, x, a[4]);
         void* s = a[4] == Py_None ? c10::cuda::getCurrentCUDAStream(x.get_device()).stream() : stream_of(a[4]);
         call("spqt_token_logprobs", [&] {
             return spqt_token_logprobs(x.data_ptr(), t == at::kHalf ? SPQT_LOGITS_FP16 : t == at::kBFloat16 ? SPQT_LOGITS_BF16 : SPQT_LOGITS_FP32,
