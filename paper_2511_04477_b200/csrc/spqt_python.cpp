@@ -173,7 +173,7 @@ struct Zigzag {
     }
 };
 
-// Runs the library call without the GIL (a launch can wait for room in the stream's queue).
+// Runs the library call without the GIL (a launch can wait for room in the stream's queue): `f` raises nothing.
 template <class F>
 void call(const char* where, F f)
 {
@@ -507,9 +507,10 @@ PyObject* kv_append(PyObject*, Args a, Py_ssize_t na)
         const at::Tensor& ws = p.tensor(a[3], at::kByte, "workspace");
         const void* counts = p.optional(a[4], {p.c->batch}, "counts");
         void* out = p.optional(a[5], {p.c->batch, p.c->kv_heads}, "length_out");
+        const int tokens = in_int(k.size(1), "the number of tokens");
         void* s = p.stream(a[6]);
         call("spqt_kv_append", [&] {
-            return spqt_kv_append(p.c, k.data_ptr(), v.data_ptr(), in_int(k.size(1), "the number of tokens"), batch_stride(k), token_stride(k),
+            return spqt_kv_append(p.c, k.data_ptr(), v.data_ptr(), tokens, batch_stride(k), token_stride(k),
                                   static_cast<const int32_t*>(counts), static_cast<int32_t*>(out), ws.data_ptr(), (size_t)ws.numel(), s);
         });
         Py_RETURN_NONE;
@@ -526,10 +527,11 @@ PyObject* kv_read(PyObject*, Args a, Py_ssize_t na)
         if (k.size(1) != v.size(1) || k.strides() != v.strides()) raise(PyExc_ValueError, "%s", "k and v must have the same shape and strides");
         const at::Tensor& ws = p.tensor(a[3], at::kByte, "workspace");
         const void* length = p.optional(a[4], {p.c->batch, p.c->kv_heads}, "length");
+        const int tokens = in_int(k.size(1), "the number of tokens");
         void* s = p.stream(a[5]);
         call("spqt_kv_read", [&] {
-            return spqt_kv_read(p.c, static_cast<const int32_t*>(length), k.data_ptr(), v.data_ptr(), in_int(k.size(1), "the number of tokens"),
-                                batch_stride(k), token_stride(k), k.size(2) > 1 ? k.stride(2) : 0, ws.data_ptr(), (size_t)ws.numel(), s);
+            return spqt_kv_read(p.c, static_cast<const int32_t*>(length), k.data_ptr(), v.data_ptr(), tokens, batch_stride(k), token_stride(k),
+                                k.size(2) > 1 ? k.stride(2) : 0, ws.data_ptr(), (size_t)ws.numel(), s);
         });
         Py_RETURN_NONE;
     });
@@ -546,6 +548,7 @@ PyObject* kv_attention(PyObject*, Args a, Py_ssize_t na)
         const float scale = a[3] == Py_None ? (float)(1.0 / std::sqrt((double)p.c->head_dim)) : float_of(a[3]);
         const int accumulate = PyObject_IsTrue(a[4]);
         if (accumulate < 0) throw Raised();
+        const int heads = in_int(q.size(2), "the number of heads"), queries = in_int(q.size(1), "the number of queries");
         at::Tensor out;
         if (a[5] == Py_None) {
             out = empty(q.sizes(), at::kHalf, q, a[6]);
@@ -555,9 +558,8 @@ PyObject* kv_attention(PyObject*, Args a, Py_ssize_t na)
         }
         void* s = p.stream(a[6]);
         call("spqt_kv_attention", [&] {
-            return spqt_kv_attention(p.c, q.data_ptr(), batch_stride(q), token_stride(q), in_int(q.size(2), "the number of heads"),
-                                     in_int(q.size(1), "the number of queries"), scale, accumulate, out.data_ptr(), batch_stride(out), token_stride(out),
-                                     ws.data_ptr(), (size_t)ws.numel(), s);
+            return spqt_kv_attention(p.c, q.data_ptr(), batch_stride(q), token_stride(q), heads, queries, scale, accumulate, out.data_ptr(),
+                                     batch_stride(out), token_stride(out), ws.data_ptr(), (size_t)ws.numel(), s);
         });
         return hand_back(a[5], out);
     });
@@ -593,7 +595,7 @@ PyObject* token_logprobs(PyObject*, Args a, Py_ssize_t na)
         if (t != at::kHalf && t != at::kBFloat16 && t != at::kFloat) raise(PyExc_TypeError, "%s must be float16, bfloat16 or float32", "logits");
         if (x.dim() != 2 || (x.size(1) > 1 && x.stride(1) != 1)) raise(PyExc_ValueError, "%s", "logits must be [rows][vocab] with unit column stride");
         const c10::cuda::OptionalCUDAGuard guard(x.device());
-        const int64_t rows = x.size(0);
+        const int rows = in_int(x.size(0), "the number of rows"), vocab = in_int(x.size(1), "the vocabulary");
         const int top = int_of(a[2]);
         if (top < 0) raise(PyExc_ValueError, "%s", "top must not be negative");
         const int wants_entropy = PyObject_IsTrue(a[3]);
@@ -612,7 +614,7 @@ PyObject* token_logprobs(PyObject*, Args a, Py_ssize_t na)
         void* s = a[4] == Py_None ? c10::cuda::getCurrentCUDAStream(x.get_device()).stream() : stream_of(a[4]);
         call("spqt_token_logprobs", [&] {
             return spqt_token_logprobs(x.data_ptr(), t == at::kHalf ? SPQT_LOGITS_FP16 : t == at::kBFloat16 ? SPQT_LOGITS_BF16 : SPQT_LOGITS_FP32,
-                                       in_int(rows, "the number of rows"), in_int(x.size(1), "the vocabulary"), rows > 1 ? x.stride(0) : x.size(1), tokens, top,
+                                       rows, vocab, rows > 1 ? x.stride(0) : vocab, tokens, top,
                                        wants_logprob ? static_cast<float*>(logprob.data_ptr()) : nullptr, wants_entropy ? static_cast<float*>(entropy.data_ptr()) : nullptr,
                                        top > 0 ? static_cast<float*>(best.data_ptr()) : nullptr, top > 0 ? static_cast<int32_t*>(index.data_ptr()) : nullptr, s);
         });

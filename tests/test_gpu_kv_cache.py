@@ -389,3 +389,17 @@ def test_cache_objects_refuse_what_does_not_fit():
     with pytest.raises(spqt.SpqtError) as e:
         spqt.new_kv_workspace(spqt.KVCache.new(1, 1, 64, 24, 1, 1), 1)
     assert e.value.status == 2
+
+
+def test_more_tokens_or_rows_than_a_whole_number_counts_are_refused():
+    """Views of one row; an error, with the interpreter's lock held when it is raised."""
+    c, w = plain_cache([70], 1, 16, 6, seed=2, weight=HEAVY)
+    ws = spqt.new_kv_workspace(c, 1)
+    row = torch.zeros((1, 1, 1, 64), dtype=torch.float16, device="cuda")
+    many = row.expand(1, 2 ** 31, 1, 64)
+    before = spqt.spqt_launch_count()
+    for call in (lambda: spqt.spqt_kv_append(c, many, many, ws), lambda: spqt.spqt_kv_read(c, many, many, ws), lambda: spqt.spqt_kv_attention(c, many, ws, out=row),
+                 lambda: spqt.spqt_token_logprobs(row.view(1, 64).expand(2 ** 31, 64))):
+        with pytest.raises(ValueError, match="too large"):
+            call()
+    assert spqt.spqt_launch_count() == before
