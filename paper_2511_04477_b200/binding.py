@@ -626,6 +626,9 @@ for _name in KVCache.TENSORS:
 
 def new_kv_workspace(cache: KVCache, q_heads: int, queries: int = 1) -> torch.Tensor:
     """Zeroed workspace of the cache's calls with at most these queries (zeroed once; calls that may overlap need two)."""
+    for name, n in (("q_heads", q_heads), ("queries", queries)):
+        if not -2 ** 31 <= n < 2 ** 31:                 # (ctypes would cut it)
+            raise ValueError("%s does not fit 32 bits" % name)
     out = ctypes.c_size_t(0)
     _ok(lib().spqt_kv_workspace(cache.desc, q_heads, queries, ctypes.byref(out)), "spqt_kv_workspace")
     return torch.zeros(int(out.value), dtype=torch.uint8, device=cache.k_codes.device)

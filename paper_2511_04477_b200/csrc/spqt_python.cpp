@@ -67,21 +67,41 @@ const at::Tensor& tensor_attr(PyObject* p, PyObject* attr, at::ScalarType dtype,
     return tensor_of(o, dtype, name);
 }
 
-int int_attr(PyObject* p, PyObject* attr)
+// A whole number of 32 bits: one that has more is refused, not cut.
+int in_int(int64_t v, const char* name)
 {
-    PyObject* o = PyObject_GetAttr(p, attr);
-    if (!o) throw Raised();
-    const long v = PyLong_AsLong(o);
-    Py_DECREF(o);
-    if (v == -1 && PyErr_Occurred()) throw Raised();
+    if (v > 0x7fffffffLL) raise(PyExc_ValueError, "%s is too large", name);
     return (int)v;
 }
 
-int int_of(PyObject* o)
+int int_of(PyObject* o, const char* name)
 {
-    const long v = PyLong_AsLong(o);
-    if (v == -1 && PyErr_Occurred()) throw Raised();
+    int beyond = 0;
+    const long v = PyLong_AsLongAndOverflow(o, &beyond);
+    if (v == -1 && !beyond && PyErr_Occurred()) throw Raised();
+    if (beyond || v != (int)v) raise(PyExc_ValueError, "%s does not fit 32 bits", name);
     return (int)v;
+}
+
+int int_attr(PyObject* p, PyObject* attr, const char* name)
+{
+    PyObject* o = PyObject_GetAttr(p, attr);
+    if (!o) throw Raised();
+    int v;
+    try {
+        v = int_of(o, name);
+    } catch (const Raised&) {
+        Py_DECREF(o);
+        throw;
+    }
+    Py_DECREF(o);
+    return v;
+}
+
+// Distance of two rows of a matrix; of one row, whose distance to the next may be anything, its length where that is too large.
+int row_stride(const at::Tensor& t, const char* name)
+{
+    return in_int(t.size(0) == 1 && t.stride(0) > 0x7fffffffLL ? t.size(1) : t.stride(0), name);
 }
 
 float float_of(PyObject* o)
@@ -168,7 +188,7 @@ struct Zigzag {
     explicit Zigzag(PyObject* p)
         : codes(tensor_attr(p, g_names.codes, at::kByte, "codes").data_ptr()),
           scale_zero(tensor_attr(p, g_names.scale_zero, at::kHalf, "scale_zero").data_ptr()),
-          m(int_attr(p, g_names.m)), n(int_attr(p, g_names.n)), bits(int_attr(p, g_names.bits)), group(int_attr(p, g_names.group))
+          m(int_attr(p, g_names.m, "m")), n(int_attr(p, g_names.n, "n")), bits(int_attr(p, g_names.bits, "bits")), group(int_attr(p, g_names.group, "group"))
     {
     }
 };
@@ -205,12 +225,12 @@ PyObject* sparsify(PyObject*, Args a, Py_ssize_t na)
         need_args(na, 5);
         const at::Tensor& x = tensor_of(a[0], at::kHalf, "x");
         const float t = float_of(a[1]);
-        const int64_t n = x.numel();
+        const int n = in_int(x.numel(), "the number of entries");
         at::Tensor idx = given_or_empty(a[2], {n > 0 ? n : 1}, at::kInt, "idx", x, a[4]);
         at::Tensor count = given_or_empty(a[3], {1}, at::kInt, "count", x, a[4]);
         if (idx.numel() < n) raise(PyExc_ValueError, "%s", "idx must hold n entries");
         void* s = stream_of(a[4]);
-        call("spqt_sparsify", [&] { return spqt_sparsify(x.data_ptr(), (int)n, t, (int32_t*)idx.data_ptr(), (int32_t*)count.data_ptr(), s); });
+        call("spqt_sparsify", [&] { return spqt_sparsify(x.data_ptr(), n, t, (int32_t*)idx.data_ptr(), (int32_t*)count.data_ptr(), s); });
         return tuple_of(hand_back(a[2], idx), hand_back(a[3], count));
     });
 }
@@ -303,14 +323,15 @@ PyObject* sparse_gemm_small(PyObject*, Args a, Py_ssize_t na)
         const Zigzag p(a[0]);
         at::Tensor Y = batch_output(p, a[1], a[6], a[7]);
         const at::Tensor& X = THPVariable_Unpack(a[1]);
+        const int ldx = row_stride(X, "the row stride of X"), ldy = row_stride(Y, "the row stride of Y");
         const float t = float_of(a[2]);
         const at::Tensor& ws = tensor_of(a[3], at::kByte, "workspace");
         at::Tensor idx = given_or_empty(a[4], {p.n}, at::kInt, "idx", X, a[7]);
         at::Tensor count = given_or_empty(a[5], {1}, at::kInt, "count", X, a[7]);
         void* s = stream_of(a[7]);
         call("spqt_sparse_gemm_small", [&] {
-            return spqt_sparse_gemm_small(p.codes, p.scale_zero, p.m, p.n, p.bits, p.group, X.data_ptr(), (int)X.stride(0), (int)X.size(0), t,
-                                          (int32_t*)idx.data_ptr(), (int32_t*)count.data_ptr(), Y.data_ptr(), (int)Y.stride(0), ws.data_ptr(),
+            return spqt_sparse_gemm_small(p.codes, p.scale_zero, p.m, p.n, p.bits, p.group, X.data_ptr(), ldx, (int)X.size(0), t,
+                                          (int32_t*)idx.data_ptr(), (int32_t*)count.data_ptr(), Y.data_ptr(), ldy, ws.data_ptr(),
                                           (size_t)ws.numel(), s);
         });
         return tuple_of(hand_back(a[6], Y), hand_back(a[4], idx), hand_back(a[5], count));
@@ -325,11 +346,12 @@ PyObject* dense_gemm_small(PyObject*, Args a, Py_ssize_t na)
         const Zigzag p(a[0]);
         at::Tensor Y = batch_output(p, a[1], a[3], a[4]);
         const at::Tensor& X = THPVariable_Unpack(a[1]);
+        const int ldx = row_stride(X, "the row stride of X"), ldy = row_stride(Y, "the row stride of Y");
         const at::Tensor& ws = tensor_of(a[2], at::kByte, "workspace");
         void* s = stream_of(a[4]);
         call("spqt_dense_gemm_small", [&] {
-            return spqt_dense_gemm_small(p.codes, p.scale_zero, p.m, p.n, p.bits, p.group, X.data_ptr(), (int)X.stride(0), (int)X.size(0),
-                                         Y.data_ptr(), (int)Y.stride(0), ws.data_ptr(), (size_t)ws.numel(), s);
+            return spqt_dense_gemm_small(p.codes, p.scale_zero, p.m, p.n, p.bits, p.group, X.data_ptr(), ldx, (int)X.size(0),
+                                         Y.data_ptr(), ldy, ws.data_ptr(), (size_t)ws.numel(), s);
         });
         return hand_back(a[3], Y);
     });
@@ -344,7 +366,7 @@ PyObject* kqw_gemv(PyObject*, Args a, Py_ssize_t na)
         PyObject* p = a[0];
         const Args rest = a + (LIST ? 4 : 2);   // workspace, y, stream, where
         const void* records = tensor_attr(p, g_names.records, at::kByte, "records").data_ptr();
-        const int m = int_attr(p, g_names.m), n = int_attr(p, g_names.n), bits = int_attr(p, g_names.bits);
+        const int m = int_attr(p, g_names.m, "m"), n = int_attr(p, g_names.n, "n"), bits = int_attr(p, g_names.bits, "bits");
         const at::Tensor& x = tensor_of(a[1], at::kHalf, "x");
         at::Tensor y = given_or_empty(rest[1], {m}, at::kHalf, "y", x, rest[2]);
         const at::Tensor& ws = tensor_of(rest[0], at::kByte, "workspace");
@@ -383,12 +405,13 @@ PyObject* pack(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         need_args(na, 4);
         const at::Tensor& W = weights_of(a[0]);
-        const int m = (int)W.size(0), n = (int)W.size(1), bits = int_of(a[1]), group = int_of(a[2]);
+        const int m = in_int(W.size(0), "the number of rows"), n = in_int(W.size(1), "the number of columns"), ldw = row_stride(W, "the row stride of W");
+        const int bits = int_of(a[1], "bits"), group = int_of(a[2], "group");
         size_t cb = 0, sb = 0;
         check(spqt_packed_sizes(m, n, bits, group, &cb, &sb, nullptr), "spqt_packed_sizes");
         at::Tensor codes = empty({(int64_t)cb}, at::kByte, W, a[3]), sz = empty({(int64_t)(sb / 2)}, at::kHalf, W, a[3]);
         void* s = stream_of(a[3]);
-        call("spqt_pack", [&] { return spqt_pack(W.data_ptr(), m, n, (int)W.stride(0), bits, group, codes.data_ptr(), sz.data_ptr(), s); });
+        call("spqt_pack", [&] { return spqt_pack(W.data_ptr(), m, n, ldw, bits, group, codes.data_ptr(), sz.data_ptr(), s); });
         return tuple_of(hand_back(Py_None, codes), hand_back(Py_None, sz));
     });
 }
@@ -399,14 +422,15 @@ PyObject* kqw_pack(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         need_args(na, 4);
         const at::Tensor& W = weights_of(a[0]);
-        const int m = (int)W.size(0), n = (int)W.size(1), bits = int_of(a[1]);
+        const int m = in_int(W.size(0), "the number of rows"), n = in_int(W.size(1), "the number of columns"), ldw = row_stride(W, "the row stride of W");
+        const int bits = int_of(a[1], "bits");
         const char* where = PyUnicode_AsUTF8(a[3]);
         if (!where) throw Raised();
         size_t rb = 0;
         check(spqt_kqw_packed_sizes(m, n, bits, &rb, nullptr), "spqt_kqw_packed_sizes");
         at::Tensor records = empty({(int64_t)rb}, at::kByte, W, a[2]);
         void* s = stream_of(a[2]);
-        call(where, [&] { return spqt_kqw_pack(W.data_ptr(), m, n, (int)W.stride(0), bits, records.data_ptr(), s); });
+        call(where, [&] { return spqt_kqw_pack(W.data_ptr(), m, n, ldw, bits, records.data_ptr(), s); });
         return hand_back(Py_None, records);
     });
 }
@@ -431,7 +455,7 @@ struct Cache {
     const spqt_kv_cache* c;
     int device;
     c10::cuda::OptionalCUDAGuard guard;
-    explicit Cache(PyObject* p) : c(nullptr), device(int_attr(p, g_names.device_index))
+    explicit Cache(PyObject* p) : c(nullptr), device(int_attr(p, g_names.device_index, "device_index"))
     {
         PyObject* o = PyObject_GetAttr(p, g_names.desc);
         if (!o) throw Raised();
@@ -475,7 +499,7 @@ struct Cache {
             PyObject* d = PyObject_GetAttr(o, g_names.device_index);
             if (d) {
                 Py_DECREF(d);
-                const int i = int_attr(o, g_names.device_index);
+                const int i = int_attr(o, g_names.device_index, "device_index");
                 if (i != device) raise(PyExc_ValueError, "%s", "the stream is another device's");
             } else {
                 PyErr_Clear();
@@ -488,12 +512,6 @@ struct Cache {
 
 int64_t batch_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
 int64_t token_stride(const at::Tensor& t) { return t.size(1) > 1 ? t.stride(1) : 0; }
-
-int in_int(int64_t v, const char* name)
-{
-    if (v > 0x7fffffffLL) raise(PyExc_ValueError, "%s is too large", name);
-    return (int)v;
-}
 
 // (cache, k, v, workspace, counts, length_out, stream) -> the lengths
 PyObject* kv_append(PyObject*, Args a, Py_ssize_t na)
@@ -571,7 +589,7 @@ PyObject* kv_evict(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         need_args(na, 8);
         const Cache p(a[0]);
-        const int keep = int_of(a[1]), first = int_of(a[2]), recent = int_of(a[3]);
+        const int keep = int_of(a[1], "keep"), first = int_of(a[2], "first"), recent = int_of(a[3], "recent");
         const at::Tensor& ws = p.tensor(a[4], at::kByte, "workspace");
         void* table = p.optional(a[5], {p.c->batch, p.c->kv_heads, p.c->table_width}, "table_out");
         void* length = p.optional(a[6], {p.c->batch, p.c->kv_heads}, "length_out");
@@ -596,7 +614,7 @@ PyObject* token_logprobs(PyObject*, Args a, Py_ssize_t na)
         if (x.dim() != 2 || (x.size(1) > 1 && x.stride(1) != 1)) raise(PyExc_ValueError, "%s", "logits must be [rows][vocab] with unit column stride");
         const c10::cuda::OptionalCUDAGuard guard(x.device());
         const int rows = in_int(x.size(0), "the number of rows"), vocab = in_int(x.size(1), "the vocabulary");
-        const int top = int_of(a[2]);
+        const int top = int_of(a[2], "top");
         if (top < 0) raise(PyExc_ValueError, "%s", "top must not be negative");
         const int wants_entropy = PyObject_IsTrue(a[3]);
         if (wants_entropy < 0) throw Raised();

@@ -403,3 +403,20 @@ def test_more_tokens_or_rows_than_a_whole_number_counts_are_refused():
         with pytest.raises(ValueError, match="too large"):
             call()
     assert spqt.spqt_launch_count() == before
+
+
+@pytest.mark.parametrize("number", [2 ** 31, 2 ** 32, 2 ** 32 + 1, -2 ** 31 - 1, -2 ** 32, 2 ** 63, -2 ** 70])
+def test_numbers_beyond_32_bits_are_refused(number):
+    c, w = plain_cache([70], 1, 16, 6, seed=2, weight=HEAVY)
+    ws = spqt.new_kv_workspace(c, 1)
+    table = c.table.clone()
+    before = spqt.spqt_launch_count()
+    x = torch.zeros((2, 40), device="cuda")
+    W = torch.zeros((256, 256), dtype=torch.float16, device="cuda")
+    for call in (lambda: spqt.spqt_kv_evict(c, number, ws), lambda: spqt.spqt_kv_evict(c, 3, ws, first=number), lambda: spqt.spqt_kv_evict(c, 3, ws, recent=number),
+                 lambda: spqt.spqt_token_logprobs(x, top=number), lambda: spqt.spqt_pack(W, number, 128), lambda: spqt.spqt_pack(W, 4, number),
+                 lambda: spqt.new_kv_workspace(c, number), lambda: spqt.new_kv_workspace(c, 1, number)):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert spqt.spqt_launch_count() == before and c.length.tolist() == [[70]] and torch.equal(c.table, table)
