@@ -667,7 +667,11 @@ def spqt_kv_evict(cache: KVCache, keep: int, workspace: torch.Tensor, first: int
 def spqt_kv_status(workspace: torch.Tensor, stream=None) -> int:
     """The status word of the cache's calls: 0, or 3 where contents of the cache were refused.  Synchronises."""
     out = ctypes.c_int(-1)
-    rc = lib().spqt_kv_status(_dev(workspace, torch.uint8, "workspace"), ctypes.byref(out), _stream(stream))
+    at = _dev(workspace, torch.uint8, "workspace")
+    if workspace.numel() < 256:
+        raise ValueError("workspace is smaller than any that new_kv_workspace gives")
+    with torch.cuda.device(workspace.device):           # (whose current stream is waited for)
+        rc = lib().spqt_kv_status(at, ctypes.byref(out), _stream(stream))
     return _status_word(rc, out, "spqt_kv_status")
 
 

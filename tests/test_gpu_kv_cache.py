@@ -420,3 +420,17 @@ def test_numbers_beyond_32_bits_are_refused(number):
             call()
     torch.cuda.synchronize()
     assert spqt.spqt_launch_count() == before and c.length.tolist() == [[70]] and torch.equal(c.table, table)
+
+
+def test_the_status_of_what_is_no_workspace_is_refused():
+    for size in (0, 4, 255):
+        with pytest.raises(ValueError):
+            spqt.spqt_kv_status(torch.zeros(size, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(TypeError):
+        spqt.spqt_kv_status(torch.zeros(256, dtype=torch.uint8))
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    assert spqt.spqt_kv_status(ws) == 0
+    ws.view(torch.int32)[63] = 3
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    assert spqt.spqt_kv_status(ws) == 3 and spqt.spqt_kv_status(ws, stream=s) == 3
