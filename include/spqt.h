@@ -554,7 +554,8 @@ spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void
 /*
  * The cache as fp16, code * scale rounded once: token t of stream (b, h) to k + b * batch_stride + t * token_stride +
  * h * head_stride (16-byte aligned, strides multiples of 8), the same for v.  Tokens from `tokens` on are left out, rows behind a
- * stream's last token stay as they were.  `length` NULL: the cache's.
+ * stream's last token stay as they were.  `length` NULL: the cache's.  No two rows may share a place: ordered by size, each stride has
+ * room for all that the smaller ones reach, and k and v are head_dim values apart or more (SPQT_ERR_INVALID_ARG otherwise).
  */
 spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void* k, void* v, int tokens, long long batch_stride,
                          long long token_stride, long long head_stride, void* workspace, size_t workspace_bytes, void* stream);
@@ -572,7 +573,7 @@ spqt_status spqt_kv_workspace(const spqt_kv_cache* cache, int q_heads, int queri
  * head (one call adds to each weight once, so that the sums do not depend on an order).  Sums and the softmax are held in fp32, p
  * enters the product to 2^-22 of the largest.  At most 64 query heads per kv head.
  *   workspace : spqt_kv_workspace bytes, 16-byte aligned, zeroed once by the caller.  Calls that may overlap need two.
- *   out must not overlap q or the cache.
+ *   out must not overlap q or the cache; its rows (q_heads * head_dim values) may not share a place either, by their strides as above.
  */
 spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long long q_batch_stride, long long q_token_stride, int q_heads,
                               int queries, float scale, int accumulate, void* out, long long out_batch_stride,

@@ -1217,6 +1217,8 @@ spqt_status spqt_kv_attention(const spqt_kv_cache* cache, const void* q, long lo
     if (!aligned(q, 16) || !aligned(out, 16) || q_batch_stride % 8 || q_token_stride % 8 || out_batch_stride % 8 || out_token_stride % 8) return SPQT_ERR_ALIGNMENT;
     st = check_kv_workspace(workspace, workspace_bytes, accumulate ? w.bytes : w.lse);
     if (st != SPQT_OK) return st;
+    RowStride strides[] = {{out_batch_stride, cache->batch}, {out_token_stride, queries}};
+    if (!rows_apart((long long)q_heads * cache->head_dim, strides)) return SPQT_ERR_INVALID_ARG;
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     const int group = q_heads / cache->kv_heads, rows = group * queries, R = rows_of(rows, (long long)cache->batch * cache->kv_heads);
     const AttnArgs a = {*cache, static_cast<const __half*>(q), q_batch_stride, q_token_stride, static_cast<__half*>(out), out_batch_stride, out_token_stride,

@@ -602,6 +602,9 @@ spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int most = cache->table_width * cache->block_tokens;
     if (tokens > most) tokens = most;
+    RowStride strides[] = {{batch_stride, cache->batch}, {token_stride, tokens}, {head_stride, cache->kv_heads}};
+    const long long apart = (static_cast<const char*>(k) - static_cast<const char*>(v)) / 2;
+    if (!rows_apart(cache->head_dim, strides) || (apart < cache->head_dim && -apart < cache->head_dim)) return SPQT_ERR_INVALID_ARG;
     const ReadArgs a = {*cache, length ? length : cache->length, static_cast<__half*>(k), static_cast<__half*>(v), tokens, batch_stride, token_stride,
                         head_stride, static_cast<int*>(status_word(workspace))};
     // (warps: at most 2^17 pieces of a row of the table times 2^14 streams)

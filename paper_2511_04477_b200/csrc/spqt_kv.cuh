@@ -2,6 +2,8 @@
 // Included after spqt_common.cuh and spqt_gemv_device.cuh.
 #pragma once
 
+#include <algorithm>
+
 namespace spqt {
 
 constexpr int kCacheRefused = 3;        // status word: a length, a count or a block number outside its range
@@ -34,6 +36,25 @@ inline spqt_status check_kv_workspace(const void* workspace, size_t bytes, size_
     if (!workspace) return SPQT_ERR_INVALID_ARG;
     if (!aligned(workspace, 16)) return SPQT_ERR_ALIGNMENT;
     return bytes < need ? SPQT_ERR_WORKSPACE : SPQT_OK;
+}
+
+// Rows of `row` values that are written, along some strides (of extents above one): whether each stride, in the order of their size,
+// has room for all that the smaller ones reach, so that no two rows share a place.
+struct RowStride {
+    long long stride;
+    int extent;
+};
+template <int N>
+inline bool rows_apart(long long row, RowStride (&s)[N])
+{
+    std::sort(s, s + N, [](const RowStride& a, const RowStride& b) { return a.stride < b.stride; });
+    __int128 reach = row;
+    for (const RowStride& d : s) {
+        if (d.extent <= 1) continue;
+        if (d.stride < reach) return false;
+        reach += (__int128)d.stride * (d.extent - 1);
+    }
+    return true;
 }
 
 __device__ __forceinline__ void refuse(int* status) { *status = kCacheRefused; }   // (all writers write the same)

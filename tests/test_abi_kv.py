@@ -111,3 +111,35 @@ def test_logprobs_arguments_that_are_refused(L, a16):
     assert lp(x=a16 + 1) == 3 and lp(x=a16 + 2, dtype=2) == 3 and lp(entropy=a16 + 2) == 3 and lp(index=a16 + 2) == 3
     assert lp(rows=0) == 0
     assert binding.spqt_launch_count() == n
+
+
+def test_rows_to_write_that_lie_on_one_another_are_refused(L, a16):
+    """Refused before a launch (which has no GPU here: a call that is not refused reports SPQT_ERR_CUDA, 5, at most)."""
+    d = desc(a16)                                        # 2 sequences, 4 kv heads of 128
+    ws, n = size(L, d, 8, 16)[1], binding.spqt_launch_count()
+
+    def read(bs, ts, hs, tokens=3, k=a16, v=a16 + (1 << 20)):
+        return L.spqt_kv_read(ctypes.byref(d), None, k, v, tokens, bs, ts, hs, a16, 4096, None)
+
+    def attend(bs, ts, queries=5):
+        return L.spqt_kv_attention(ctypes.byref(d), a16, 0, 0, 8, queries, 1.0, 0, a16 + (1 << 20), bs, ts, a16, ws, None)
+    far = 2 ** 62
+    for bad in ((0, 512, 128), (1536, 0, 128), (1536, 512, 0), (1536, 512, 120), (1536, 504, 128), (1528, 512, 128), (512, 512, 128), (128, 512, 128), (512, 1024, 1024),
+                (far, 512, 64)):
+        assert read(*bad) == 1, bad
+    assert read(1536, 512, 128, k=a16, v=a16) == 1 and read(1536, 512, 128, v=a16 + 240) == 1 and read(1536, 512, 128, k=a16 + 240, v=a16) == 1
+    assert read(1024, 0, 128, tokens=2) == 1
+    for bad in ((0, 1024), (5120 - 8, 1024), (1024, 1024), (1016, 8192), (8192, 1016), (8192, 0)):
+        assert attend(*bad) == 1, bad
+    assert attend(1016, 0, queries=1) == 1
+    assert binding.spqt_launch_count() == n
+    one = desc(a16, batch=1, kv_heads=1)
+    if binding.torch.cuda.is_available():
+        return                                           # (the addresses are not real: the calls that are taken stay off the GPU)
+    for good in ((1536, 512, 128), (4096, 1024, 256), (512, 1024, 128), (1536, 128, 384), (128, 1024, 256), (far, 512, 128)):
+        assert read(*good) == 5, good
+    assert read(1536, 512, 128, v=a16 + 256) == 5 and read(512, 0, 128, tokens=1) == 5
+    assert L.spqt_kv_read(ctypes.byref(one), None, a16, a16 + 4096, 1, 0, 0, 0, a16, 4096, None) == 5
+    for good in ((5120, 1024), (1024, 2048), (far, 1024)):
+        assert attend(*good) == 5, good
+    assert attend(1024, 0, queries=1) == 5
