@@ -560,7 +560,8 @@ spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void
 spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void* k, void* v, int tokens, long long batch_stride,
                          long long token_stride, long long head_stride, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace that the cache's calls need with at most `q_heads` and `queries` (q_heads a multiple of kv_heads). */
+/* Bytes of workspace that the cache's calls need with at most `q_heads` and `queries` (q_heads a multiple of kv_heads).  The rows of a
+ * stream, queries * q_heads / kv_heads, go by sixteen: batch * kv_heads * ceil(rows / 16) <= 16384 (SPQT_ERR_UNSUPPORTED otherwise). */
 spqt_status spqt_kv_workspace(const spqt_kv_cache* cache, int q_heads, int queries, size_t* bytes);
 
 /*
@@ -571,7 +572,7 @@ spqt_status spqt_kv_workspace(const spqt_kv_cache* cache, int q_heads, int queri
  * at out + b * out_batch_stride + i * out_token_stride + g * head_dim (16-byte aligned, strides multiples of 8).  A query that sees
  * no token gives zeros.  accumulate != 0: weight of token t += the sum of p_t over the queries and over the query heads of its kv
  * head (one call adds to each weight once, so that the sums do not depend on an order).  Sums and the softmax are held in fp32, p
- * enters the product to 2^-22 of the largest.  At most 64 query heads per kv head.
+ * enters the product to 2^-22 of the largest.  At most 64 query heads per kv head, and the limit on rows of spqt_kv_workspace.
  *   workspace : spqt_kv_workspace bytes, 16-byte aligned, zeroed once by the caller.  Calls that may overlap need two.
  *   out must not overlap q or the cache; its rows (q_heads * head_dim values) may not share a place either, by their strides as above.
  */

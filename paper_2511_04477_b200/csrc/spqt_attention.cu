@@ -1020,16 +1020,18 @@ struct AttnWorkspace {
     size_t arrived, begin, ml, o, lse, tiles, scores, bytes;   // (what stays zero between calls at a place that depends on nothing)
 };
 
-// false where the tiles' numbers would pass 31 bits
 constexpr int kMoreTiles = 8;           // tiles of 16 tokens of a block of 128, the largest
 inline int most_tiles(const spqt_kv_cache& c) { return (c.table_width * c.block_tokens + kTile - 1) / kTile + kMoreTiles; }
+static_assert((long long)kMaxStreams * (kMaxTableWidth * 128 / kTile + kMoreTiles + kRoom) <= 0x7fffffffLL, "a tile's number in 31 bits, whatever the cache");
+
+// false where there are more segments than counts of parts
 inline bool attention_workspace(const spqt_kv_cache& c, int group, int queries, AttnWorkspace* w)
 {
     const long long streams = (long long)c.batch * c.kv_heads;
     const int rows = group * queries, R = rows_of(rows, streams), groups = (rows + R - 1) / R;
     const long long segments = streams * groups;
-    const long long tiles = segments * ((long long)most_tiles(c) + kRoom);
-    if (segments > kMaxStreams || tiles > 0x7fffffffLL) return false;
+    if (segments > kMaxStreams) return false;
+    const long long tiles = segments * (most_tiles(c) + kRoom);
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     size_t at = kKvHeader;
     w->arrived = at, at += (size_t)kMaxStreams * 4;

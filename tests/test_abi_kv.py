@@ -143,3 +143,20 @@ def test_rows_to_write_that_lie_on_one_another_are_refused(L, a16):
     for good in ((5120, 1024), (1024, 2048), (far, 1024)):
         assert attend(*good) == 5, good
     assert attend(1024, 0, queries=1) == 5
+
+
+def test_the_joint_limit_of_streams_and_rows(L, a16):
+    """batch * kv_heads * ceil(rows / 16) <= 16384 and nothing else refuses a cache within the single limits."""
+    for batch, kv_heads, group, queries in ((4096, 4, 1, 16), (4096, 4, 16, 1), (4096, 4, 1, 1), (8192, 1, 2, 16), (8191, 1, 32, 1), (256, 1, 64, 16), (255, 1, 64, 16),
+                                            (1, 16, 64, 16), (4096, 2, 3, 10), (1, 256, 64, 16)):
+        assert size(L, desc(a16, batch=batch, kv_heads=kv_heads), kv_heads * group, queries)[0] == 0
+    for batch, kv_heads, group, queries in ((4096, 4, 17, 1), (4096, 4, 2, 9), (8193, 1, 2, 16), (257, 1, 64, 16), (8192, 1, 4, 16), (4096, 2, 3, 16)):
+        d = desc(a16, batch=batch, kv_heads=kv_heads)
+        assert size(L, d, kv_heads * group, queries)[0] == 2
+        assert L.spqt_kv_attention(ctypes.byref(d), a16, 0, 0, kv_heads * group, queries, 1.0, 0, a16, 0, 0, a16, 1 << 40, None) == 2
+    # the largest cache there is: its tiles and scores are counted in 64 bits
+    largest = desc(a16, batch=1, kv_heads=16384, table_width=16384, block_tokens=128, head_dim=256, blocks=2 ** 31 - 1)
+    rc, n = size(L, largest, 16384 * 16)
+    tiles = 16384 * (16384 * 128 // 32 + 8 + 16)
+    assert rc == 0 and n > tiles * (16 + 32 * 16 * 4)
+    assert size(L, desc(a16, batch=1024, kv_heads=16, table_width=16384, block_tokens=128, weight=None), 16)[0] == 0
