@@ -552,7 +552,8 @@ spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void
                            size_t workspace_bytes, void* stream);
 
 /*
- * The cache as fp16, code * scale rounded once: token t of stream (b, h) to k + b * batch_stride + t * token_stride +
+ * The cache as fp16, the product of code and scale in fp32 rounded to fp16 (two roundings: the second meets a tie that the first has
+ * made for a few values, which are then a step of fp16 from the exact product's nearest neighbour): token t of stream (b, h) to k + b * batch_stride + t * token_stride +
  * h * head_stride (16-byte aligned, strides multiples of 8), the same for v.  Tokens from `tokens` on are left out, rows behind a
  * stream's last token stay as they were.  `length` NULL: the cache's.  No two rows may share a place: ordered by size, each stride has
  * room for all that the smaller ones reach, and k and v are head_dim values apart or more (SPQT_ERR_INVALID_ARG otherwise).

@@ -434,3 +434,33 @@ def test_the_status_of_what_is_no_workspace_is_refused():
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     assert spqt.spqt_kv_status(ws) == 3 and spqt.spqt_kv_status(ws, stream=s) == 3
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_read_is_the_product_in_fp32_rounded_to_fp16(fmt):
+    """Every code with scales that append gives, of blocks of the smallest to the largest maxima, bit for bit."""
+    top = 127.0 if fmt == "int8" else 448.0
+    maxima = np.array([m * 2.0 ** e for e in range(-24, 16, 3) for m in (1.0, 1.25, 1.875, 1.9990234375)] + [2.0 ** -10, 65504.0, 0.0])
+    maxima = maxima[maxima <= 65504].astype(np.float16)
+    scale = (maxima.astype(np.float64) / top).astype(np.float32)
+    blocks, bt, dim = len(scale), 16, 64
+    codes = np.resize(np.arange(256, dtype=np.uint8), (blocks, bt, dim))
+    codes[(codes & 127) == 127 if fmt == "e4m3" else codes == 128] = 0       # (not-a-number; -128, which no append writes)
+    c = spqt.KVCache.new(1, 1, dim, bt, blocks, blocks, dtype=DTYPE[fmt])
+    c.table.copy_(torch.arange(blocks, dtype=torch.int32).view(1, 1, -1))
+    c.length.fill_(blocks * bt)
+    for t in (c.k_codes, c.v_codes):
+        t.view(torch.uint8).copy_(dev(codes))
+    for t in (c.k_scale, c.v_scale):
+        t.copy_(dev(scale))
+    k, v = (torch.empty((1, blocks * bt, 1, dim), dtype=torch.float16, device="cuda") for _ in range(2))
+    ws = spqt.new_kv_workspace(c, 1)
+    spqt.spqt_kv_read(c, k, v, ws)
+    exact = from_codes(codes, scale, fmt)
+    want = exact.astype(np.float32).astype(np.float16)
+    for got in (k, v):
+        assert np.array_equal(got.cpu().numpy().view(np.uint16).reshape(want.shape), want.view(np.uint16))
+    once = exact.astype(np.float16)
+    step = np.maximum(np.abs(exact) * 2.0 ** -10, 2.0 ** -24)
+    assert (np.abs(want.astype(np.float64) - once.astype(np.float64)) <= step).all()
+    assert fmt == "int8" or (want != once).any()         # 7 * 2^-9 with the scale of 2^-10: 0, of which the nearest is 2^-24
