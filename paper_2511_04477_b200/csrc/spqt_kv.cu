@@ -253,12 +253,12 @@ cudaError_t launch_append(const AppendArgs& a, cudaStream_t s)
     const dim3 grid((unsigned)a.c.kv_heads, (unsigned)(touched < most ? touched : most), (unsigned)a.c.batch);
     // threads for one of k and v: a multiple of a warp and of a row's pieces
     constexpr int kUnit = D == 96 ? 96 : 32;
-    if (pieces <= 2048) {
-        const int half = (pieces / 4 + kUnit - 1) / kUnit * kUnit;
-        if (half <= 128) return launch_overlapping(kv_append_kernel<FMT, D, 4, 256>, grid, 2 * half, 0, s, a);
-        return launch_overlapping(kv_append_kernel<FMT, D, 4, 1024>, grid, 2 * half, 0, s, a);
+    if constexpr (D == 256) {                       // (blocks of 128 tokens: eight pieces a thread)
+        if (pieces > 2048) return launch_overlapping(kv_append_kernel<FMT, D, 8, 1024>, grid, 1024, 0, s, a);
     }
-    return launch_overlapping(kv_append_kernel<FMT, D, 8, 1024>, grid, 1024, 0, s, a);
+    const int half = (pieces / 4 + kUnit - 1) / kUnit * kUnit;
+    if (half <= 128) return launch_overlapping(kv_append_kernel<FMT, D, 4, 256>, grid, 2 * half, 0, s, a);
+    return launch_overlapping(kv_append_kernel<FMT, D, 4, 1024>, grid, 2 * half, 0, s, a);
 }
 
 // ---------------------------------------------------------------- the cache as fp16

@@ -27,7 +27,7 @@ namespace {
 PyObject* g_error = nullptr;   // binding.SpqtError(status, where)
 
 struct Names {
-    PyObject *codes, *scale_zero, *records, *m, *n, *bits, *group, *cuda_stream, *desc, *device_index, *device;
+    PyObject *codes, *scale_zero, *records, *m, *n, *bits, *group, *cuda_stream, *desc, *device_index;
 } g_names;
 
 // Leaves a call with a Python exception set.
@@ -670,6 +670,6 @@ PyMODINIT_FUNC PyInit__native(void)
     g_names = {PyUnicode_InternFromString("codes"), PyUnicode_InternFromString("scale_zero"), PyUnicode_InternFromString("records"),
                PyUnicode_InternFromString("m"), PyUnicode_InternFromString("n"), PyUnicode_InternFromString("bits"),
                PyUnicode_InternFromString("group"), PyUnicode_InternFromString("cuda_stream"), PyUnicode_InternFromString("desc"),
-               PyUnicode_InternFromString("device_index"), PyUnicode_InternFromString("device")};
+               PyUnicode_InternFromString("device_index")};
     return PyModule_Create(&g_module);
 }

@@ -464,3 +464,11 @@ def test_read_is_the_product_in_fp32_rounded_to_fp16(fmt):
     step = np.maximum(np.abs(exact) * 2.0 ** -10, 2.0 ** -24)
     assert (np.abs(want.astype(np.float64) - once.astype(np.float64)) <= step).all()
     assert fmt == "int8" or (want != once).any()         # 7 * 2^-9 with the scale of 2^-10: 0, of which the nearest is 2^-24
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("bt", [16, 32, 64, 128])
+def test_append_of_every_head_and_block_size(fmt, dim, bt):
+    """Every launch shape that there is, and no other: the largest block has eight pieces a thread."""
+    test_append(fmt, dim, bt, bt + 3)
