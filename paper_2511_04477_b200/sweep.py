@@ -463,11 +463,13 @@ def run_decode(layers=32, context=8192, keep=2048, tokens=96, block=32, sparsity
             attn_out_thr.append(float(binding.spqt_calibrate_threshold(att.view(-1), sparsity, stream=s)))
         step(s, True, attn_out_thr)                      # the token that fills the context's last block; down to the budget
     torch.cuda.synchronize()
-    graphs = []
+    graphs, launches = [], []
     for evict in (False, True):
         gph = torch.cuda.CUDAGraph()
+        before = binding.spqt_launch_count()
         with torch.cuda.graph(gph, stream=s):
             step(s, evict, attn_out_thr)
+        launches.append(binding.spqt_launch_count() - before)
         graphs.append((gph, answers[:]))
     tokens = max(block, tokens // block * block)
     e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
@@ -486,7 +488,7 @@ def run_decode(layers=32, context=8192, keep=2048, tokens=96, block=32, sparsity
     cached = keep + block / 2
     read = layers * KV * cached * (2 * D + 8 + 12 / block)
     out = {"layers": layers, "context": context, "budget_tokens": keep, "tokens": tokens, "ms_per_token": ms, "tokens_per_s": 1e3 / ms,
-           "launches_per_token": layers * (4 + 3 + 1 / block) + 2, "cache_mb_read_per_token": read * 1e-6,
+           "launches_per_token": ((block - 1) * launches[0] + launches[1]) / block, "cache_mb_read_per_token": read * 1e-6,
            "cache_bytes_per_token_of_context": 2 * D * KV * layers, "length": max(n), "logprob": float(logprob[0]), "entropy": float(entropy[0]),
            "top_index": index[0].tolist(), "device_status": status}
     assert min(n) == max(n) == keep, n

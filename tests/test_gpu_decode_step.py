@@ -178,3 +178,23 @@ def test_the_first_calls_of_a_process_can_be_captured():
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS_IN_A_GRAPH], capture_output=True, text=True, timeout=300,
                        cwd=pathlib.Path(__file__).resolve().parents[1])
     assert r.returncode == 0 and r.stdout.strip() == "same", r.stdout + r.stderr
+
+
+def test_the_decode_workload_counts_its_launches():
+    """What it says of launches is what one layer's calls launch: four linears, append, attention (weights added in the same
+    kernel here), the eviction with every block's last token; the head and the log probabilities once."""
+    from paper_2511_04477_b200 import sweep
+    layers, block = 1, 32
+    r = sweep.run_decode(layers=layers, context=512, keep=128, tokens=block, block=block)
+    c = spqt.KVCache.new(1, sweep.DECODE_HEADS["kv_heads"], sweep.DECODE_HEADS["head_dim"], block, 8 * 18, 512 // block + 2, weight=True)
+    ws = spqt.new_kv_workspace(c, sweep.DECODE_HEADS["q_heads"])
+    q = torch.zeros((1, 1, sweep.DECODE_HEADS["q_heads"], sweep.DECODE_HEADS["head_dim"]), dtype=torch.float16, device="cuda")
+    k = q[:, :, :sweep.DECODE_HEADS["kv_heads"]]
+    c.table.copy_(torch.arange(8 * 18, dtype=torch.int32).view(1, 8, 18))
+    counts = []
+    for call in (lambda: spqt.spqt_kv_append(c, k, k, ws), lambda: spqt.spqt_kv_attention(c, q, ws, accumulate=True), lambda: spqt.spqt_kv_evict(c, 4, ws)):
+        before = spqt.spqt_launch_count()
+        call()
+        counts.append(spqt.spqt_launch_count() - before)
+    torch.cuda.synchronize()
+    assert abs(r["launches_per_token"] - (layers * (4 + counts[0] + counts[1] + counts[2] / block) + 2)) < 1e-9
