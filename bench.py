@@ -309,8 +309,9 @@ def other_config_line(which, local, quick=False):
                         result=res)
         elif which == "decode":
             res = sweep.run_decode(layers=8 if quick else 32, peak=peak)
-            line = dict(base, metric="tokens/s of whole decode steps, 32-layer Llama-3-8B-shaped stack, int4 g128, 40% sparsity, 8-bit cache bounded "
-                                     "by accumulated attention",
+            line = dict(base, metric="tokens/s of the linear layers, 8-bit cache, attention, head and log probabilities of decode steps (no normalisation, "
+                                     "rotation, activation, residual sum or sampling), %d-layer Llama-3-8B-shaped stack, int4 g128, 40%% sparsity, cache "
+                                     "bounded by accumulated attention" % res["layers"],
                         unit="tokens/s", value=res["tokens_per_s"], ms_per_step=res["ms_per_token"], steps=res["tokens"], warmup=32,
                         config={"workload": "%d layers x (q|k|v, cache append, attention with weights, o, gate|up, down), dense head 128256x4096 and log "
                                             "probabilities; context 8192, cut to 2048 tokens' blocks of 32 with every full block; one CUDA graph per kind of token"

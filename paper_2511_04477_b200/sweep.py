@@ -1,4 +1,5 @@
-"""The benchmark's other workloads: sparsity sweep, format sweep, dense shape sweep, the 32-layer stack and its whole decode steps.
+"""The benchmark's other workloads: sparsity sweep, format sweep, dense shape sweep, the 32-layer stack alone and with cache,
+attention, head and log probabilities.
 
 Used by ``bench.py --config sweep|formats|dense|stack|decode`` (and, in reduced form, by its default line).
 Each case packs several distinct weight copies (together well above the 126 MB L2), visits them
@@ -400,11 +401,12 @@ DECODE_VOCAB = 128256
 
 
 def run_decode(layers=32, context=8192, keep=2048, tokens=96, block=32, sparsity=0.4, peak=None):
-    """Whole decode steps of the stack at batch 1: in every layer q | k | v, the new key and value into the layer's 8-bit cache,
+    """Of decode steps of the stack at batch 1: in every layer q | k | v, the new key and value into the layer's 8-bit cache,
     attention over it with the weights accumulated, o, gate | up and down, then the head (dense) and the log probability, entropy
-    and alternatives of the token.  The cache holds `context` tokens at the beginning and between `keep` and `keep` plus
+    and alternatives of the token.  Not in it: normalisation, rotation, activation, residual sums, sampling; every linear but o and
+    the head reads the same input at every token (their time does not depend on its values, so that all new keys are alike).  The cache holds `context` tokens at the beginning and between `keep` and `keep` plus
     a block afterwards: with every block that becomes full all but the `keep` tokens' blocks of largest accumulated weight leave
-    (the first and the last four always stay).  One graph per kind of token, replayed; lengths and tables live on the device, so
+    (the first and the last four always stay; the first time, when the context is cut, one query has left weights).  One graph per kind of token, replayed; lengths and tables live on the device, so
     that a replay is the next token."""
     peak = peak or hbm_peak()[0]
     H, KV, D = (DECODE_HEADS[k] for k in ("q_heads", "kv_heads", "head_dim"))
