@@ -496,8 +496,9 @@ spqt_status spqt_probe_arith(int chunks_per_warp, float* sink, size_t sink_float
                              unsigned long long* chunks_total, void* stream);
 
 /* ------------------------------------------------------------------------------------------------------------------------
- * The rest of a decode step: a cache of keys and values in 8 bits, attention over it, its eviction, and what a caller asks of the
- * logits.  (No counterpart in the paper, whose path is the linears; these stand between q|k|v and o, and behind the last one.)
+ * What a decode step needs beside its linears: a cache of keys and values in 8 bits, attention over it, its eviction, and what a
+ * caller asks of the logits.  (No counterpart in the paper, whose path is the linears; these stand between q|k|v and o, and behind
+ * the last one.  Normalisation, rotation, activations, residual sums and sampling are the caller's.)
  *
  * The cache.  A sequence b and a kv head h are a stream of tokens.  It owns blocks of `block_tokens` tokens in a pool, named in
  * order by its row of `table`: token t lies in pool block table[b][h][t / block_tokens].  A block that is full is held as 8-bit
@@ -546,6 +547,10 @@ typedef struct {
  * become full are rounded, the rest stays in the tail, the tokens' weights become 0, and the new lengths go to `length_out`
  * (int32[batch][kv_heads]; NULL: in place of the old ones).  A stream whose tokens would not fit its row of the table, or of whose
  * touched blocks one lies outside the pool, is left as it was, and the status word says so.
+ *   With length_out the buffers change as without: the cache then is what it is with the new lengths, not with the old ones.
+ *   Weights are of queries that have been asked for: after a prompt was appended all its weights are 0, and an eviction would keep the
+ * earliest blocks, as of equal sums.  The caller writes the weights of the prompt's own attention to `weight`, or has its last queries
+ * go through spqt_kv_attention (16 at a time) first.
  */
 spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void* v, int tokens, long long batch_stride,
                            long long token_stride, const int32_t* counts, int32_t* length_out, void* workspace,
@@ -555,7 +560,8 @@ spqt_status spqt_kv_append(const spqt_kv_cache* cache, const void* k, const void
  * The cache as fp16, the product of code and scale in fp32 rounded to fp16 (two roundings: the second meets a tie that the first has
  * made for a few values, which are then a step of fp16 from the exact product's nearest neighbour): token t of stream (b, h) to k + b * batch_stride + t * token_stride +
  * h * head_stride (16-byte aligned, strides multiples of 8), the same for v.  Tokens from `tokens` on are left out, rows behind a
- * stream's last token stay as they were.  `length` NULL: the cache's.  No two rows may share a place: ordered by size, each stride has
+ * stream's last token stay as they were.  `length` NULL: the cache's; else lengths that spqt_kv_append or spqt_kv_evict wrote elsewhere
+ * (not shorter ones: the length says which tokens are in the tail).  No two rows may share a place: ordered by size, each stride has
  * room for all that the smaller ones reach, and k and v are head_dim values apart or more (SPQT_ERR_INVALID_ARG otherwise).
  */
 spqt_status spqt_kv_read(const spqt_kv_cache* cache, const int32_t* length, void* k, void* v, int tokens, long long batch_stride,
@@ -571,7 +577,8 @@ spqt_status spqt_kv_workspace(const spqt_kv_cache* cache, int q_heads, int queri
  * the tokens t < length - queries + 1 + i of its stream:
  *   out = sum_t p_t v_t,  p = softmax over t of scale * <q, k_t>
  * at out + b * out_batch_stride + i * out_token_stride + g * head_dim (16-byte aligned, strides multiples of 8).  A query that sees
- * no token gives zeros.  accumulate != 0: weight of token t += the sum of p_t over the queries and over the query heads of its kv
+ * no token gives zeros.  (The queries end with the sequence: one with fewer new tokens than `queries` has its own at the end and padding
+ * in front.)  accumulate != 0: weight of token t += the sum of p_t over the queries and over the query heads of its kv
  * head (one call adds to each weight once, so that the sums do not depend on an order).  Sums and the softmax are held in fp32, p
  * enters the product to 2^-22 of the largest.  At most 64 query heads per kv head, and the limit on rows of spqt_kv_workspace.
  *   workspace : spqt_kv_workspace bytes, 16-byte aligned, zeroed once by the caller.  Calls that may overlap need two.
@@ -602,8 +609,8 @@ spqt_status spqt_kv_status(const void* workspace, int* status_host, void* stream
  *   top_logprob[r][i], top_index[r][i], i < top: the largest log probabilities and their places, descending, of equal logits the
  *   lower place first.
  * Sums in fp32.  logits: rows of `vocab` values, `row_stride` values apart, aligned to their type.  `tokens` NULL: no logprob; a
- * token outside [0, vocab) gives not-a-number.  entropy NULL: not computed.  A logit of -infinity has probability 0; a row with
- * not-a-number, +infinity, or -infinity alone gives not-a-number (the places are still those of the largest logits, not-a-number
+ * token outside [0, vocab) gives not-a-number.  entropy NULL: not computed.  A logit of -infinity, or so far below the largest that its
+ * exponential is 0, has probability 0; a row with not-a-number, +infinity, or -infinity alone gives not-a-number (the places are still those of the largest logits, not-a-number
  * above all).  top <= 32, top <= vocab <= 1048576.
  */
 enum { SPQT_LOGITS_FP16 = 0, SPQT_LOGITS_BF16 = 1, SPQT_LOGITS_FP32 = 2 };

@@ -5,9 +5,10 @@
 //
 // The product runs transposed on mma.sync.m16n8k16: A is the codes, 16 tokens (or 16 dimensions of v) an instruction, B the
 // queries (or the probabilities), eight rows; with few rows the tensor cores are there for their operand format, and the other
-// orientation would fill its 16 rows with nothing.  tcgen05 does not fit: codes would have to be widened to 16 bits through
-// shared memory first, twice the bytes of the codes themselves in and out again.  An 8-bit code becomes an exact fp16 value in
-// registers (a byte permutation and a subtraction, or one conversion from e4m3).  Scales stay outside of the product: a block's k scale multiplies its scores,
+// orientation would fill its 16 rows with nothing.  An 8-bit code becomes an exact fp16 value in registers (a byte permutation and a
+// subtraction, or one conversion from e4m3), and with four to sixteen rows that is most of a tile's instructions (of 780 with four
+// rows 32 are products), tensor pipe 17 % at most.  tcgen05 would not change that: its A may come from tensor memory, which takes
+// the widened values from registers, 16 bits each, on top.  Scales stay outside of the product: a block's k scale multiplies its scores,
 // its v scale the probabilities.
 //
 // Probabilities are needed in fp16: p = 2^(s + e - M + 10), s the score in powers of two, 2^e the power of two in the v scale, M the

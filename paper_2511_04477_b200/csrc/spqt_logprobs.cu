@@ -581,8 +581,9 @@ cudaError_t launch_logprobs(LogArgs a, int rows, cudaStream_t s)
             const int teams = 256 / team, grid = (rows - 1) / teams + 1;
             return launch_overlapping(kernel, dim3(grid < 4 * sms ? grid : 4 * sms), 256, 0, s, a, rows);
         };
-        // 2000 x 8000 fp16, top 20, a warp / 128 threads a row: 24.3 / 19.3 us; 4096 x 8000: 22.4 / 31.1; 1000 x 2000: 5.7 / 7.0; 1000 x 4000: 13.5 / 8.1.
-        // 128 / 256 threads: 2048 x 32000 42.5 / 44.7; 512 x 128256 48.8 / 37.1
+        // fp16, a warp / 128 threads a row, top 5 and top 20: 1000 x 2000 5.6 / 7.1 and 9.1 / 7.7 us; 4000 x 2000 9.6 / 23.1 and 15.7 / 25.0;
+        // 1000 x 4000 9.7 / 7.9 and 11.2 / 8.4; 2000 x 8000 16.1 / 16.7 and 21.3 / 18.3; 4096 x 8000 24.0 / 31.7 and 30.1 / 34.7.
+        // 128 / 256 threads, top 20: 2048 x 32000 38.3 / 46.2; 512 x 128256 37.9 / 34.7
         if (a.vocab <= 2048 || (a.vocab <= 8192 && rows >= 16 * sms)) return rows_by(token_logprobs_rows_kernel<T, 32>, 32);
         if ((size_t)a.vocab * sizeof(T) <= 65536) return rows_by(token_logprobs_rows_kernel<T, 128>, 128);
         return rows_by(token_logprobs_rows_kernel<T, 256>, 256);
