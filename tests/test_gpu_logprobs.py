@@ -245,3 +245,5 @@ def test_as_many_rows_as_a_whole_number_counts():
         found += (nan.nonzero().flatten() + at).tolist()
         assert bool((nan | (part == 0)).all())
     assert found == odd
+    del buf, entropy, part, nan
+    torch.cuda.empty_cache()
