@@ -9,8 +9,8 @@
 //
 // The largest `top` of a part: every warp names the largest few of its threads' maxima, and the top-th largest of those named is a
 // bound that `top` values or more reach, hardly more in most rows.  Only the threads that reach it have their values looked at again;
-// these are listed, and each finds its place by counting those before it.  Where more reach the bound than the list holds
-// (many equal ones), the top-th value is searched bit by bit.  Equal values count in the order of their places throughout: a value
+// these are listed, and each finds its place by counting those before it.  Where more reach the bound than the list holds, those above
+// it are listed and the first of those equal to it; where too many are above it, the top-th value is searched bit by bit.  Equal values count in the order of their places throughout: a value
 // and its place are one number.
 #include <cuda_bf16.h>
 
@@ -314,6 +314,65 @@ struct LogTeam {
         const int at = atomicAdd(&sh.listed[turn], 1);
         if (at < LIST) sh.list[at] = k;
     }
+    static __device__ __forceinline__ bool overfull(const int& count) { return *reinterpret_cast<volatile const int*>(&count) > LIST; }
+    // More values reach the bound than the list holds.  In a row whose other values are masked most of them are the bound itself: the
+    // values above it are listed, and of those equal to it the first `top` of each warp's share of the part, of which the first of all
+    // are some.  (Where too many are above it the list is left overfull.)  A call, with few arguments:
+    // the team's own registers are those of the rows.  8 x 128256 with all but 50 values masked 190 us when the
+    // top-th key was searched for at once, 2048 x 32000 with all but 10, top 20, 7.8 ms.
+    static __device__ __noinline__ void list_beside_equal(LogShared<NW, LIST>& sh, const T* row, int n, int tid, int turn, int top, float floor)
+    {
+        const LogPart<T> p(row, n);
+        const int lane = tid & 31, warp = tid >> 5;
+        int& count = sh.listed[turn];
+        auto put = [&](unsigned long long k) {
+            const int at = atomicAdd(&count, 1);
+            if (at < LIST) sh.list[at] = k;
+        };
+        if (tid < p.odd && !(sh.odd[tid] < floor)) put(key_of(sh.odd[tid], p.place_of_odd(tid)));
+        float lo, hi;
+#pragma unroll 1
+        for (int i = tid; i < p.vecs && !overfull(count); i += TEAM) {
+            const Vec<T> w(ld_global_v4(p.vec(i)));
+#pragma unroll
+            for (int e = 0; e < Vec<T>::P; ++e) {
+                w.pair(e, lo, hi);
+                if (!(lo <= floor)) put(key_of(lo, p.head + i * V + 2 * e));        // (not-a-number is above)
+                if (!(hi <= floor)) put(key_of(hi, p.head + i * V + 2 * e + 1));
+            }
+        }
+        sync();
+        const bool room = count + NW * top <= LIST;
+        sync();
+        if (!room) {
+            if (tid == 0) count = LIST + 1;
+            return;
+        }
+        const int share = (p.vecs + NW - 1) / NW, end = min(p.vecs, (warp + 1) * share);
+        int found = 0;
+#pragma unroll 1
+        for (int i0 = warp * share; i0 < end && found < top; i0 += 32) {
+            const int i = i0 + lane;
+            unsigned same = 0u;                                 // which of the vector's values
+            if (i < end) {
+                const Vec<T> w(ld_global_v4(p.vec(i)));
+#pragma unroll
+                for (int e = 0; e < Vec<T>::P; ++e) {
+                    w.pair(e, lo, hi);
+                    same |= (lo == floor ? 1u : 0u) << (2 * e) | (hi == floor ? 2u : 0u) << (2 * e);
+                }
+            }
+            const int mine = __popc(same);
+            int until = mine;                                   // in this lane and those before it
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, until, o);
+                if (lane >= o) until += v;
+            }
+            for (int at = found + until - mine; same != 0u && at < top; same &= same - 1u, ++at) put(key_of(floor, p.head + i * V + __ffs(same) - 1));
+            found += __shfl_sync(0xffffffffu, until, 31);
+        }
+    }
     // The sums of the warps and, in order, the part's `top` largest keys (places within the part), for the first warp.
     __device__ __forceinline__ void finish(const LogPart<T>& p)
     {
@@ -377,6 +436,7 @@ struct LogTeam {
             const int k = sh.who[x >> shift], v = x & ((1 << shift) - 1);
             const int i = ((k / TEAM << slot_shift) + (v >> 2)) * (TEAM * kVecs) + (v & 3) * TEAM + k % TEAM;
             if (i >= p.vecs) continue;
+            if (pairs > LIST / 2 && overfull(sh.listed[turn])) break;   // (they are looked at anew below; few pairs are through sooner)
             const Vec<T> w(ld_global_v4(p.vec(i)));
             float lo, hi, any = 0.0f;
 #pragma unroll
@@ -396,6 +456,14 @@ struct LogTeam {
         if (tid < p.odd && !(sh.odd[tid] < floor)) put(key_of(sh.odd[tid], p.place_of_odd(tid)));
         sync();
         int listed = sh.listed[turn];
+        if (listed > LIST && least != 0u) {                    // (every warp has the same bound)
+            sync();
+            if (tid == 0) sh.listed[turn] = 0;
+            sync();
+            list_beside_equal(sh, p.row, p.odd + p.vecs * V, tid, turn, a.top, floor);
+            sync();
+            listed = sh.listed[turn];
+        }
         if (listed > LIST) {                                    // the top-th largest key, bit by bit
             // each value of the part with its place
             auto each_key = [&](auto f) {

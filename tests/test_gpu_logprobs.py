@@ -247,3 +247,49 @@ def test_as_many_rows_as_a_whole_number_counts():
     assert found == odd
     del buf, entropy, part, nan
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("top", [1, 20, 32])
+def test_more_values_equal_to_the_bound_than_a_list_holds(dtype, shape, top):
+    """Filtered logits: few values, or none, above those that are all alike; these in front, behind, everywhere or in a stretch, with a
+    lower value elsewhere."""
+    rows, vocab = SHAPES[shape][dtype == "fp32"]
+    rows = max(rows, 12)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(51)
+    x = torch.empty((rows, vocab), dtype=TYPES[dtype], device="cuda")
+    inf = float("inf")
+    for r in range(rows):
+        alike, lower = [(-inf, -inf), (-65504.0, -inf), (0.5, -3.0), (-0.0, -inf)][r % 4]
+        x[r] = alike
+        if r % 3 == 1:
+            x[r, :vocab // 2] = lower                    # the equal ones at the end
+        elif r % 3 == 2:
+            x[r] = lower
+            x[r, vocab // 3:2 * vocab // 3] = alike
+        keep = [0, 1, 3, 19, 50, 200][r % 6]
+        at = torch.randperm(vocab, generator=g, device="cuda")[:keep]
+        x[r, at] = (torch.randn(keep, generator=g, device="cuda").abs() * 3 + 1).to(TYPES[dtype])
+        if alike == -inf and keep == 0:
+            x[r, vocab - 1] = 2.0
+    x[3, 5] = 0.0                                        # a zero of the other sign is equal too
+    check_shifted(x, torch.full((rows,), vocab - 1, dtype=torch.int32, device="cuda"), top)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+def test_more_values_above_the_bound_than_a_list_holds(dtype, shape):
+    """The largest values all in the hands of a few threads, whose other maxima are low, so that the bound is low as well."""
+    rows, vocab = SHAPES[shape][dtype == "fp32"]
+    per = {"warp": 32, "team": 128, "cta": 256, "cluster": 512}[shape] * (16 if dtype == "fp16" else 8) // 2
+    x = torch.full((rows, vocab), -1.0, dtype=TYPES[dtype], device="cuda")
+    place = torch.arange(vocab, device="cuda")
+    hands = (place % per) < (64 if shape != "warp" else 96)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(52)
+    x = torch.where(hands, torch.randn((rows, vocab), generator=g, device="cuda").to(TYPES[dtype]) * 2 + 9, x)
+    x[:, 1::2] = torch.where(hands[1::2], x[:, 1::2], torch.full_like(x[:, 1::2], -2.0))
+    for top in (5, 32):
+        check_shifted(x, torch.zeros(rows, dtype=torch.int32, device="cuda"), top)
